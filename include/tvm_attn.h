@@ -10,7 +10,8 @@
  * Conventions for every entry point
  *   - All tensor pointers are DEVICE pointers on the current device, owned by the caller, 16-byte
  *     aligned, (B, H, rows, d) with d contiguous: packed by default, with the strides given in
- *     tvm_attn_params otherwise.  Row statistics are packed (B, H, M) float.  The library never
+ *     tvm_attn_params otherwise.  (The operators on rows of the model width, further down, state their own
+ *     layouts and alignments.)  Row statistics are packed (B, H, M) float.  The library never
  *     allocates, frees or keeps device memory.
  *   - Outputs are fully overwritten, never accumulated into.
  *   - Work is enqueued on `cuda_stream` (a cudaStream_t passed as void*; NULL = default stream)
@@ -185,6 +186,89 @@ int tvm_qk_rmsnorm_jvp_bwd(const tvm_attn_params* p, float eps, const void* Q, c
                            const void* tK, const float* gQ, const float* gK, const void* dQn, const void* dtQn,
                            const void* dKn, const void* dtKn, void* dQ, void* dtQ, void* dK, void* dtK,
                            float* dgQ, float* dgK, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Rows of the model width: the norm in front of the attention of the paper's transformer, and the projections around the
+ * attention in a sampler.
+ *
+ * A tensor of rows is (B, T, D): element strides between the rows of a batch and between batches (both zero: packed), the D
+ * elements of a row contiguous.  Rows do not overlap: row >= D where T > 1, batch >= D where B > 1.  Every tensor of a call has
+ * strides of its own.  A null tvm_attn_rows* or a null ptr in it is an absent tensor.  Rows that begin on 16 bytes (pointer
+ * and strides multiples of 16 bytes, and of 8 for 8-bit rows; D a multiple of 16 bytes; a 16-byte aligned scale) are read and
+ * written 16 bytes at a time, others element by element (and their sums added up in another order).  Pointers are aligned to their element.
+ * An output may be one of the call's inputs of the same type, with the same strides; otherwise outputs overlap nothing.
+ * B = 0 or T = 0 is a call without rows (TVM_ATTN_OK).
+ */
+#define TVM_ATTN_MAX_WIDTH 16384
+typedef struct {
+    void* ptr;
+    int64_t row, batch;
+} tvm_attn_rows;
+typedef struct {
+    int32_t B, T, D;    /* 1 <= D <= TVM_ATTN_MAX_WIDTH (TVM_ATTN_UNSUPPORTED beyond), B * T < 2^31 */
+    int32_t dtype;      /* TVM_ATTN_BF16 or TVM_ATTN_FP32 */
+    float eps;          /* >= 0 */
+} tvm_attn_rows_params;
+
+/*
+ * RMSNorm of a sum, with a tangent (paper Sec. 4 "semi-Lipschitz control": RMSNorm in place of LayerNorm; App. "Lipschitzness of
+ * RMSNorm" for the Jacobian J v = (v - u (u . v) / D) / r):
+ *     h = x + res    r = sqrt(mean(h^2) + eps)    u = h / r    y = g * u
+ *     th = tx + tres                              ty = g * (J th)
+ * The norm is that of the unrounded sum.  The sums over a row are fp32; rows whose squares leave its range are scaled first.
+ *   in : x; res or absent (h = x); tx or absent (no tangents); tres or absent (th = tx), only with tx
+ *        g: D floats or NULL (no learnable scale)
+ *   out: y; h exactly where res is given; ty exactly where tx is; th exactly where tres is
+ */
+int tvm_attn_rmsnorm_jvp_fwd(const tvm_attn_rows_params* p, const tvm_attn_rows* x, const tvm_attn_rows* res, const tvm_attn_rows* tx,
+                             const tvm_attn_rows* tres, const float* g, const tvm_attn_rows* y, const tvm_attn_rows* h,
+                             const tvm_attn_rows* ty, const tvm_attn_rows* th, void* cuda_stream);
+
+/*
+ * Backward through all outputs of tvm_attn_rmsnorm_jvp_fwd.  With the cotangents dy, dty of y, ty and dh, dth of h, th:
+ *     dtx = J (g * dty) + dth     dx = J (g * dy) + d/dh [ (g * dty) . (J(h) th) ] + dh
+ *     dg = sum over the rows of dy * u + dty * (J th)
+ * dx is the gradient of x and of res, dtx that of tx and of tres.
+ *   in : h (what the forward wrote, or its x without a residual); dy; dh or absent (zero);
+ *        th and dty, both or neither (neither: no tangents, or a loss that does not use ty); dth or absent, only with th
+ *   out: dx; dtx exactly where th is given; dg: D floats exactly where g is given, written, bit-reproducible
+ *   workspace: at least tvm_attn_rmsnorm_jvp_workspace_bytes(p) bytes, 16-byte aligned, where g is given (partial sums of
+ *        dg); calls that may overlap on the device have one each.  0 is returned for invalid parameters.
+ */
+size_t tvm_attn_rmsnorm_jvp_workspace_bytes(const tvm_attn_rows_params* p);
+int tvm_attn_rmsnorm_jvp_bwd(const tvm_attn_rows_params* p, const tvm_attn_rows* h, const tvm_attn_rows* dy, const tvm_attn_rows* dh,
+                             const tvm_attn_rows* th, const tvm_attn_rows* dty, const tvm_attn_rows* dth, const float* g,
+                             const tvm_attn_rows* dx, const tvm_attn_rows* dtx, float* dg, void* workspace, size_t workspace_bytes,
+                             void* cuda_stream);
+
+/*
+ * The same norm without tangents, its output in 8 bits with a scale for each row: h = x + res, y = g h / r,
+ *     s = max|y| / 127     q = y / s rounded to nearest even (a row of zeros: s = 0, q = 0)
+ * A row that holds an infinity or a NaN gets q = 0 and an s that is not finite, so that its products are not finite either.
+ *   in : x, res or absent, g or NULL (as above)      out: q: 8-bit rows; s: B * T floats, packed; h exactly where res is given
+ */
+int tvm_attn_rmsnorm_s8(const tvm_attn_rows_params* p, const tvm_attn_rows* x, const tvm_attn_rows* res, const float* g,
+                        const tvm_attn_rows* q, float* s, const tvm_attn_rows* h, void* cuda_stream);
+
+/* Rows to 8 bits without a norm, s = max|x| / 127 (activations by token, weights by output channel); eps is not used. */
+int tvm_attn_quantize_s8(const tvm_attn_rows_params* p, const tvm_attn_rows* x, const tvm_attn_rows* q, float* s, void* cuda_stream);
+
+/*
+ * Product of 8-bit rows with 8-bit weights:
+ *     y[m, n] = s[m] * ws[n] * sum_k q[m, k] w[n, k] + bias[n]
+ * The sum is exact; the scaling is fp32, rounded once to the output's type.
+ *   in : q (M, K), w (N, K) signed 8-bit integers (-128 too); s: M floats, ws: N floats; bias: N floats or NULL
+ *   out: y (M, N) of `dtype`
+ * K <= 65536 (TVM_ATTN_UNSUPPORTED beyond).  Rows of q and w begin on 16 bytes: pointers 16-byte aligned, ldq and ldw multiples
+ * of 16 and >= K (what lies between K and ldq is not read).  y is aligned to its element, ldy >= N.  M = 0 is a call without rows.
+ */
+typedef struct {
+    int32_t M, N, K;
+    int32_t dtype;            /* of y: TVM_ATTN_BF16 or TVM_ATTN_FP32 */
+    int64_t ldq, ldw, ldy;    /* elements between rows; 0: K, K, N */
+} tvm_attn_linear_params;
+int tvm_attn_linear_s8(const tvm_attn_linear_params* p, const void* q, const float* s, const void* w, const float* ws, const float* bias,
+                       void* y, void* cuda_stream);
 
 /*
  * Synchronises `cuda_stream` and reports what the kernels enqueued so far on the current device

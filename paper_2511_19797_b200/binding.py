@@ -29,6 +29,20 @@ class TvmAttnError(RuntimeError):
         self.code = code
 
 
+class Rows(ctypes.Structure):
+    """A (B, T, D) tensor of rows; strides in elements, both zero for a packed one."""
+    _fields_ = [("ptr", ctypes.c_void_p), ("row", ctypes.c_int64), ("batch", ctypes.c_int64)]
+
+
+class RowsParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class LinearParams(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int32), ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("ldq", ctypes.c_int64), ("ldw", ctypes.c_int64), ("ldy", ctypes.c_int64)]
+
+
 class Params(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("N", ctypes.c_int32), ("d", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("M", ctypes.c_int32),
@@ -38,10 +52,14 @@ class Params(ctypes.Structure):
 _lib = None
 _native = None
 _BOUND = ("tvm_attn_jvp_fwd", "tvm_attn_jvp_bwd", "tvm_attn_jvp_bwd_noalloc", "tvm_attn_jvp_workspace_bytes",
-          "tvm_qk_rmsnorm_jvp_fwd", "tvm_qk_rmsnorm_jvp_bwd", "tvm_qk_rmsnorm_jvp_workspace_bytes")
+          "tvm_qk_rmsnorm_jvp_fwd", "tvm_qk_rmsnorm_jvp_bwd", "tvm_qk_rmsnorm_jvp_workspace_bytes",
+          "tvm_attn_rmsnorm_jvp_fwd", "tvm_attn_rmsnorm_jvp_bwd", "tvm_attn_rmsnorm_jvp_workspace_bytes",
+          "tvm_attn_rmsnorm_s8", "tvm_attn_quantize_s8", "tvm_attn_linear_s8")
 EXPORTS = ("tvm_attn_jvp_workspace_bytes", "tvm_attn_jvp_fwd", "tvm_attn_jvp_bwd", "tvm_attn_jvp_bwd_noalloc",
            "tvm_attn_check_status", "tvm_attn_selftest_timeout",
            "tvm_qk_rmsnorm_jvp_fwd", "tvm_qk_rmsnorm_jvp_bwd", "tvm_qk_rmsnorm_jvp_workspace_bytes",
+           "tvm_attn_rmsnorm_jvp_fwd", "tvm_attn_rmsnorm_jvp_bwd", "tvm_attn_rmsnorm_jvp_workspace_bytes",
+           "tvm_attn_rmsnorm_s8", "tvm_attn_quantize_s8", "tvm_attn_linear_s8",
            "tvm_attn_launch_count", "tvm_attn_strerror", "tvm_attn_version", "tvm_attn_set_profiling",
            "tvm_attn_get_profile")
 
@@ -82,6 +100,19 @@ def load(build_if_missing=False):
     lib.tvm_qk_rmsnorm_jvp_fwd.argtypes = [pp, ctypes.c_float] + [vp] * 10 + [vp]
     lib.tvm_qk_rmsnorm_jvp_bwd.restype = ctypes.c_int
     lib.tvm_qk_rmsnorm_jvp_bwd.argtypes = [pp, ctypes.c_float] + [vp] * 16 + [vp, ctypes.c_size_t, vp]
+    rp, rr = ctypes.POINTER(RowsParams), ctypes.POINTER(Rows)
+    lib.tvm_attn_rmsnorm_jvp_workspace_bytes.restype = ctypes.c_size_t
+    lib.tvm_attn_rmsnorm_jvp_workspace_bytes.argtypes = [rp]
+    lib.tvm_attn_rmsnorm_jvp_fwd.restype = ctypes.c_int
+    lib.tvm_attn_rmsnorm_jvp_fwd.argtypes = [rp] + [rr] * 4 + [vp] + [rr] * 4 + [vp]
+    lib.tvm_attn_rmsnorm_jvp_bwd.restype = ctypes.c_int
+    lib.tvm_attn_rmsnorm_jvp_bwd.argtypes = [rp] + [rr] * 6 + [vp] + [rr] * 2 + [vp, vp, ctypes.c_size_t, vp]
+    lib.tvm_attn_rmsnorm_s8.restype = ctypes.c_int
+    lib.tvm_attn_rmsnorm_s8.argtypes = [rp, rr, rr, vp, rr, vp, rr, vp]
+    lib.tvm_attn_quantize_s8.restype = ctypes.c_int
+    lib.tvm_attn_quantize_s8.argtypes = [rp, rr, rr, vp, vp]
+    lib.tvm_attn_linear_s8.restype = ctypes.c_int
+    lib.tvm_attn_linear_s8.argtypes = [ctypes.POINTER(LinearParams)] + [vp] * 7
     lib.tvm_attn_selftest_timeout.restype = ctypes.c_int
     lib.tvm_attn_selftest_timeout.argtypes = [ctypes.c_uint64, vp]
     lib.tvm_attn_launch_count.restype = ctypes.c_uint64
@@ -175,6 +206,68 @@ def tvm_qk_rmsnorm_jvp_bwd(Q, tQ, K, tK, gQ, gK, dQn, dtQn, dKn, dtKn, eps=1e-6,
                                              None if stream is None else stream.cuda_stream)
     if r.__class__ is int:
         _raise("tvm_qk_rmsnorm_jvp_bwd", r)
+    return r
+
+
+def tvm_attn_rmsnorm_jvp_workspace_bytes(D, dtype=BF16):
+    """Bytes of workspace of tvm_attn_rmsnorm_jvp_bwd with a scale, whatever the number of rows; 0 for invalid parameters."""
+    p = RowsParams(1, 1, D, dtype, 0.0)
+    return int(load().tvm_attn_rmsnorm_jvp_workspace_bytes(ctypes.byref(p)))
+
+
+def tvm_attn_rmsnorm_jvp_fwd(x, res=None, tx=None, tres=None, g=None, eps=1e-6, out=None, stream=None):
+    """RMSNorm over the last dimension of h = x + res, with the tangent th = tx + tres: returns (y, h, ty, th).
+
+    The tensors are (..., D), bf16 or fp32, of one shape, with strides of their own (two at most for the rows); g is the
+    learnable scale, D fp32 values, or None.  Without `res`, h is x itself; without `tx`, ty and th are None; without `tres`, th is
+    tx itself.  `out` may hold preallocated (y, h, ty, th), None for those that are not computed (h without `res`, and so on); an
+    output may be an input, the residual stream updated in place for instance."""
+    r = (_native or _load_native()).rows_fwd(x, res, tx, tres, g, eps, out, None if stream is None else stream.cuda_stream)
+    if r.__class__ is int:
+        _raise("tvm_attn_rmsnorm_jvp_fwd", r)
+    return r
+
+
+def tvm_attn_rmsnorm_jvp_bwd(h, dy, th=None, dty=None, dh=None, dth=None, g=None, eps=1e-6, out=None, workspace=None, stream=None):
+    """Backward of tvm_attn_rmsnorm_jvp_fwd: returns (dx, dtx, dg) from its h and th and the cotangents of y, ty, h and th.
+
+    dx is the gradient of x and of res, dtx that of tx and of tres (None without tangents), dg that of the scale (None without
+    one).  dh and dth may be None (zero).  A loss that does not use ty leaves out th, dty and dth (dtx is then dth itself).
+    `workspace`: a uint8 CUDA tensor of tvm_attn_rmsnorm_jvp_workspace_bytes(D, dtype) bytes, used where g is given."""
+    r = (_native or _load_native()).rows_bwd(h, dy, th, dty, dh, dth, g, eps, out, workspace, None if stream is None else stream.cuda_stream)
+    if r.__class__ is int:
+        _raise("tvm_attn_rmsnorm_jvp_bwd", r)
+    return r
+
+
+def tvm_attn_rmsnorm_s8(x, res=None, g=None, eps=1e-6, out=None, stream=None):
+    """RMSNorm of h = x + res in 8 bits: returns (q, s, h), the norm's output being q * s[..., None].  q is int8 with rows that begin
+    on 16 bytes (strided where D is no multiple of 16), s has one fp32 scale for each row; without `res`, h is x itself."""
+    r = (_native or _load_native()).rows_s8(x, res, g, eps, True, out, None if stream is None else stream.cuda_stream)
+    if r.__class__ is int:
+        _raise("tvm_attn_rmsnorm_s8", r)
+    return r
+
+
+def tvm_attn_quantize_s8(x, out=None, stream=None):
+    """Rows (..., D) to 8 bits with a scale for each: returns (q, s), x being q * s[..., None] rounded.  Activations by token, or
+    weights (N, K) by output channel, once."""
+    r = (_native or _load_native()).rows_s8(x, None, None, 0.0, False, out, None if stream is None else stream.cuda_stream)
+    if r.__class__ is int:
+        _raise("tvm_attn_quantize_s8", r)
+    return r
+
+
+def tvm_attn_linear_s8(q, s, w, ws, bias=None, dtype=torch.bfloat16, out=None, stream=None):
+    """Product of 8-bit rows with 8-bit weights: returns y[..., n] = s[...] * ws[n] * sum_k q[..., k] w[n, k] + bias[n].
+
+    q (..., K) and w (N, K) are int8 with rows that begin on 16 bytes, as tvm_attn_quantize_s8 makes them; s, ws and bias are
+    fp32; `dtype` is that of the result, bfloat16 or float32."""
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise ValueError("the result is bfloat16 or float32")
+    r = (_native or _load_native()).linear_s8(q, s, w, ws, bias, dtype is torch.float32, out, None if stream is None else stream.cuda_stream)
+    if r.__class__ is int:
+        _raise("tvm_attn_linear_s8", r)
     return r
 
 

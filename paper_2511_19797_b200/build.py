@@ -11,7 +11,7 @@ _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB_DIR = os.path.join(_HERE, "_lib")
 LIB_PATH = os.path.join(LIB_DIR, "libtvm_attn.so")
-SOURCES = ["tvm_attn_api.cu"]
+SOURCES = ["tvm_attn_api.cu", "row_ops_api.cu"]
 BINDING_SOURCE = os.path.join(CSRC, "torch_binding.cpp")
 
 
@@ -26,7 +26,7 @@ def _newest_source_mtime():
 def nvcc_command(out_path, extra=()):
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     return [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-            "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(_ROOT, "include"), "-I", CSRC,
+            "-Xcompiler", "-fPIC", "-shared", "--threads", str(len(SOURCES)), "-I", os.path.join(_ROOT, "include"), "-I", CSRC,
             *extra, "-o", out_path, *[os.path.join(CSRC, s) for s in SOURCES]]
 
 

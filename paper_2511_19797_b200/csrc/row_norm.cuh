@@ -1,0 +1,485 @@
+// RMSNorm over the model width with the residual's addition and a tangent, its backward through all outputs, and its
+// 8-bit form: the norm in front of the attention of the paper's transformer (Sec. 4 "semi-Lipschitz control": LayerNorm
+// replaced by RMSNorm without a learnable scale; App. "Lipschitzness of RMSNorm" for the Jacobian).  Per row of D elements:
+//     h = x + res     r = sqrt(mean(h^2) + eps)     u = h / r     y = g u
+//     th = tx + tres                                ty = g J th   with J v = (v - u (u . v) / D) / r
+// Streaming work, every tensor read or written once.  A row stays in registers between its loads and its stores, as fp32: up to
+// 5 chunks of 16 bytes on each of P <= 32 lanes of a warp, or 3 or 4 on each thread of a block of its own.  The sums over a
+// row, the dot products and the scale's gradient are fp32.  The norm is that of the sum before it is rounded to the type
+// that h is stored in.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "chunks.cuh"
+#include "sm100_ptx.cuh"
+
+namespace tvm_attn {
+
+// Rows of a (B, T, D) tensor: element strides between the rows of a batch and between batches.
+struct RowsPtr {
+    void* p;
+    long long row, batch;
+};
+
+struct RowNormParams {
+    RowsPtr in[6];    // forward: x, res, tx, tres; backward: h, dy, dh, th, dty, dth
+    RowsPtr out[4];   // forward: y (or the 8-bit rows), h, ty, th; backward: dx, dtx
+    const float* g;   // null: no learnable scale
+    float* aux;       // 8-bit rows: their scales; backward: partial sums of the scale's gradient, or null
+    unsigned total, T;
+    int D, P;         // P: lanes of a row (all threads of the block where a row has one of its own)
+    float eps;
+    bool norm;        // 8-bit rows: of the norm's output (else of x + res itself)
+};
+
+// A warp's rows: at most this many chunks a lane; wider rows get a block.
+constexpr int ROWNORM_WARP_CHUNKS = 5;
+constexpr int ROWNORM_THREADS = 256;       // forward, rows on warps
+constexpr int ROWNORM_BWD_THREADS = 128;   // backward, rows on warps
+
+// Threads that a block with one row can have: 16384 elements at 4 chunks a thread.
+template <typename T> constexpr int rownorm_block_threads() { return 16384 * (int)sizeof(T) / 64; }
+// Blocks of the backward at most.  A fixed number: the partial sums of the scale's gradient, a row per block, have a size
+// and an order that do not depend on the device.  `warps`: of a block with one row, 0 for rows on warps.
+__host__ __device__ constexpr int rownorm_bwd_blocks(int warps) { return 148 * (warps == 0 ? 3 : warps < 12 ? 12 / warps : 1); }
+
+// The lanes of one row and their columns.  VEC: a chunk is 16 contiguous bytes.  Otherwise (a pointer, stride or width that is
+// no multiple of 16 bytes) the elements of a chunk are P apart, so that an instruction still touches contiguous bytes.
+template <typename T, bool VEC>
+struct RowLane {
+    static constexpr int V = RmsVec<T>::N;
+    int c, P, D;
+    __device__ __forceinline__ int col(int i, int e) const { return VEC ? (c + P * i) * V + e : c + P * (i * V + e); }
+    // A chunk as it lies in memory, zeros behind the row.
+    __device__ __forceinline__ uint4 raw(const T* row, bool act, int i) const {
+        uint4 q = make_uint4(0, 0, 0, 0);
+        if constexpr (VEC) {
+            if (act && col(i, 0) < D) q = *reinterpret_cast<const uint4*>(row + col(i, 0));
+        } else {
+            uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (act && col(i, e) < D) {
+                    if constexpr (V == 4) w[e] = __float_as_uint(row[col(i, e)]);
+                    else w[e / 2] |= (uint32_t)__bfloat16_as_ushort(row[col(i, e)]) << (16 * (e & 1));
+                }
+            q = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        return q;
+    }
+    __device__ __forceinline__ void load(const T* row, bool act, int i, uint64_t (&v)[V / 2]) const { rms_unpack(raw(row, act, i), v); }
+    __device__ __forceinline__ void store(T* row, int i, const uint64_t (&v)[V / 2]) const {
+        if constexpr (VEC) {
+            if (col(i, 0) < D) rms_store(row + col(i, 0), v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float a, b;
+                ptx::unpack2(v[e / 2], a, b);
+                if (col(i, e) < D) row[col(i, e)] = (T)(e & 1 ? b : a);
+            }
+        }
+    }
+    // The scale's elements for a chunk: 1 where there is no scale, 0 behind the row.
+    __device__ __forceinline__ void scale(const float* g, int i, uint64_t (&v)[V / 2]) const {
+        if (!g) {
+#pragma unroll
+            for (int e = 0; e < V / 2; ++e) v[e] = ptx::pack2(1.f, 1.f);
+        } else if constexpr (VEC) {
+#pragma unroll
+            for (int e = 0; e < V / 2; e += 2) {
+                float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (col(i, 0) < D) q = __ldg(reinterpret_cast<const float4*>(g + col(i, 2 * e)));
+                v[e] = ptx::pack2(q.x, q.y);
+                v[e + 1] = ptx::pack2(q.z, q.w);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; e += 2) v[e / 2] = ptx::pack2(col(i, e) < D ? __ldg(g + col(i, e)) : 0.f, col(i, e + 1) < D ? __ldg(g + col(i, e + 1)) : 0.f);
+        }
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ T* row_at(const RowsPtr& t, unsigned row, const RowNormParams& p) {
+    if (p.T == p.total) return static_cast<T*>(t.p) + (size_t)row * (size_t)t.row;
+    const unsigned b = row / p.T;
+    return static_cast<T*>(t.p) + (size_t)b * (size_t)t.batch + (size_t)(row - b * p.T) * (size_t)t.row;
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) {   // a NaN on either side stays
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// N sums over a row (the last one a maximum with MAX), returned to all its lanes, the same bits on each.  `slot`: shared
+// memory of a block with one row, 32 N floats; two of them are used in turn, so that one barrier a reduction is enough.
+template <int N, bool MAX, bool BLOCK>
+__device__ __forceinline__ void row_reduce(float (&v)[N], int P, float* slot) {
+    const int lanes = BLOCK ? 32 : P;
+    for (int off = lanes >> 1; off > 0; off >>= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float w = __shfl_xor_sync(0xffffffffu, v[k], off);
+            v[k] = MAX && k == N - 1 ? max_nan(v[k], w) : v[k] + w;
+        }
+    if constexpr (BLOCK) {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+        if (lane == 0)
+#pragma unroll
+            for (int k = 0; k < N; ++k) slot[32 * k + warp] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] = lane < warps ? slot[32 * k + lane] : 0.f;   // (the maximum is one of magnitudes)
+            for (int off = 16; off > 0; off >>= 1) {
+                const float w = __shfl_xor_sync(0xffffffffu, v[k], off);
+                v[k] = MAX && k == N - 1 ? max_nan(v[k], w) : v[k] + w;
+            }
+        }
+    }
+}
+
+// The power of two that a row's elements are multiplied by in its sum of squares, when that sum left the range of fp32 at `pre` =
+// 1: a second sum is then taken.  0: the sum is fine.  (With eps of ordinary size a row of tiny elements needs none.)
+__device__ __forceinline__ float row_rescale(float ss, float eps) {
+    return !(ss <= 3.0e38f) ? 0x1p-64f : ss < 1e-30f && eps < 1e-30f ? 0x1p64f : 0.f;
+}
+
+// ROW_NORM: y (h, ty, th).  ROW_NORM_TAN: with tangents.  ROW_S8: 8-bit rows q = rint(v / s), s = max|v| / 127, of v = y or x + res;
+// a row that holds an infinity or a NaN gets a scale that is not finite, and zeros.
+enum { ROW_NORM = 0, ROW_NORM_TAN = 1, ROW_S8 = 2 };
+
+template <typename T, int C, bool BLOCK, bool VEC, int MODE>
+__global__ void __launch_bounds__(BLOCK ? rownorm_block_threads<T>() : ROWNORM_THREADS, BLOCK ? 1 : 2)
+row_norm_kernel(const RowNormParams p) {
+    constexpr int V = RmsVec<T>::N;
+    constexpr bool TAN = MODE == ROW_NORM_TAN;
+    constexpr int N = MODE == ROW_NORM ? 1 : 2;
+    __shared__ float slots[BLOCK ? 2 * 32 * N : 1];
+    const int lane = threadIdx.x & 31, rpw = BLOCK ? 1 : 32 / p.P;
+    const RowLane<T, VEC> L{BLOCK ? (int)threadIdx.x : lane & (p.P - 1), BLOCK ? (int)blockDim.x : p.P, p.D};
+    const unsigned per_block = BLOCK ? 1u : (ROWNORM_THREADS / 32) * rpw;
+    const float inv_d = 1.0f / (float)p.D;
+    unsigned turn = 0;
+    auto slot = [&]() { return slots + (BLOCK ? (turn++ & 1u) * 32 * N : 0); };
+    for (unsigned base = blockIdx.x * per_block; base < p.total; base += gridDim.x * per_block) {
+        const unsigned row = BLOCK ? base : base + (threadIdx.x >> 5) * rpw + lane / p.P;
+        const bool act = BLOCK || row < p.total;
+        const unsigned at = act ? row : 0;
+        uint64_t h[C][V / 2], t[TAN ? C : 1][V / 2];
+        {
+            const T* x = row_at<const T>(p.in[0], at, p);
+#pragma unroll
+            for (int i = 0; i < C; ++i) L.load(x, act, i, h[i]);
+            if constexpr (TAN) {
+                const T* tx = row_at<const T>(p.in[2], at, p);
+#pragma unroll
+                for (int i = 0; i < C; ++i) L.load(tx, act, i, t[i]);
+            }
+            if (p.in[1].p) {
+                const T* res = row_at<const T>(p.in[1], at, p);
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    uint64_t w[V / 2];
+                    L.load(res, act, i, w);
+#pragma unroll
+                    for (int e = 0; e < V / 2; ++e) h[i][e] = ptx::add2(h[i][e], w[e]);
+                }
+            }
+            if constexpr (TAN)
+                if (p.in[3].p) {
+                    const T* tres = row_at<const T>(p.in[3], at, p);
+#pragma unroll
+                    for (int i = 0; i < C; ++i) {
+                        uint64_t w[V / 2];
+                        L.load(tres, act, i, w);
+#pragma unroll
+                        for (int e = 0; e < V / 2; ++e) t[i][e] = ptx::add2(t[i][e], w[e]);
+                    }
+                }
+        }
+        if (p.out[1].p && act) {
+            T* to = row_at<T>(p.out[1], at, p);
+#pragma unroll
+            for (int i = 0; i < C; ++i) L.store(to, i, h[i]);
+        }
+        if constexpr (TAN)
+            if (p.out[3].p && act) {
+                T* to = row_at<T>(p.out[3], at, p);
+#pragma unroll
+                for (int i = 0; i < C; ++i) L.store(to, i, t[i]);
+            }
+        // sums[0] = h . h, sums[1] = h . th or max |g h|; elements times `pre` in the first two
+        float sums[N], pre = 1.f;
+        auto sum_up = [&]() {
+            const uint64_t pre2 = ptx::pack2(pre, pre);
+            uint64_t ss2 = 0ull, s2 = 0ull;
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                uint64_t g[V / 2];
+                if constexpr (MODE == ROW_S8) L.scale(p.g, i, g);
+#pragma unroll
+                for (int e = 0; e < V / 2; ++e) {
+                    const uint64_t x = ptx::mul2(h[i][e], pre2);
+                    ss2 = ptx::fma2(x, x, ss2);
+                    if constexpr (TAN) s2 = ptx::fma2(x, t[i][e], s2);
+                    if constexpr (MODE == ROW_S8) {
+                        float a, b;
+                        ptx::unpack2(ptx::mul2(h[i][e], g[e]), a, b);
+                        top = max_nan(top, max_nan(fabsf(a), fabsf(b)));
+                    }
+                }
+            }
+            sums[0] = rms_hsum(ss2);
+            if constexpr (N > 1) sums[N - 1] = MODE == ROW_S8 ? top : rms_hsum(s2);
+            row_reduce<N, MODE == ROW_S8, BLOCK>(sums, p.P, slot());
+        };
+        sum_up();
+        const float again = row_rescale(sums[0], p.eps);
+        if (BLOCK ? again != 0.f : __any_sync(0xffffffffu, again != 0.f)) {   // (the rows of the warp that need none keep pre = 1)
+            pre = again != 0.f ? again : 1.f;
+            sum_up();
+        }
+        const float root = 1.0f / sqrtf(sums[0] * inv_d + p.eps * pre * pre);   // 1 / (r pre)
+        const float inv = root * pre;
+        if constexpr (MODE == ROW_S8) {
+            // scaled up first where 127 / max would leave the range
+            const float top = sums[N - 1], up = top < 0x1p-100f ? 0x1p100f : 1.f;
+            const float k = top > 0.f || top != top ? 127.f / (top * up) : 0.f;
+            if (act) {
+                if (L.c == 0) p.aux[row] = top * (p.norm ? inv : 1.f) / 127.f;
+                int8_t* to = row_at<int8_t>(p.out[0], at, p);
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    uint64_t g[V / 2];
+                    L.scale(p.g, i, g);
+                    int q[V];
+#pragma unroll
+                    for (int e = 0; e < V / 2; ++e) {
+                        float a, b;
+                        ptx::unpack2(ptx::mul2(h[i][e], g[e]), a, b);
+                        q[2 * e] = __float2int_rn(a * up * k);   // (not a number: 0)
+                        q[2 * e + 1] = __float2int_rn(b * up * k);
+                    }
+                    if constexpr (VEC) {
+                        uint32_t w[V / 4];
+#pragma unroll
+                        for (int e = 0; e < V / 4; ++e)
+                            w[e] = __byte_perm(__byte_perm(q[4 * e], q[4 * e + 1], 0x0040), __byte_perm(q[4 * e + 2], q[4 * e + 3], 0x0040), 0x5410);
+                        if (L.col(i, 0) < p.D) {
+                            if constexpr (V == 8) *reinterpret_cast<uint2*>(to + L.col(i, 0)) = make_uint2(w[0], w[V / 4 - 1]);
+                            else *reinterpret_cast<uint32_t*>(to + L.col(i, 0)) = w[0];
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < V; ++e)
+                            if (L.col(i, e) < p.D) to[L.col(i, e)] = (int8_t)q[e];
+                    }
+                }
+            }
+        } else if (act) {
+            const float m = TAN ? sums[N - 1] * root * root * inv_d : 0.f;   // (u . th) / (D r pre) = (u . th) root / D
+            const uint64_t inv2 = ptx::pack2(inv, inv), nm2 = ptx::pack2(-m * pre, -m * pre);
+            T* y = row_at<T>(p.out[0], at, p);
+            T* ty = TAN ? row_at<T>(p.out[2], at, p) : nullptr;
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                uint64_t g[V / 2], o[V / 2];
+                L.scale(p.g, i, g);
+#pragma unroll
+                for (int e = 0; e < V / 2; ++e) o[e] = ptx::mul2(g[e], ptx::mul2(h[i][e], inv2));
+                L.store(y, i, o);
+                if constexpr (TAN) {
+#pragma unroll
+                    for (int e = 0; e < V / 2; ++e)
+                        o[e] = ptx::mul2(g[e], ptx::fma2(ptx::mul2(h[i][e], inv2), nm2, ptx::mul2(t[i][e], inv2)));
+                    L.store(ty, i, o);
+                }
+            }
+        }
+    }
+}
+
+// Backward.  With a = g dy, b = g dty, and au = a . u, bu = b . u, ut = u . th, bt = b . th:
+//     dtx = (b - u bu / D) / r + dth
+//     dx  = (a - u au / D) / r + ((3 bu ut / D - bt) u - ut b - bu th) / (D r^2) + dh
+//     dg  = sum over the rows of dy u + dty J th
+// dx is the gradient of x and of the residual alike.  Every thread keeps the dg terms of its own columns over the rows it
+// walks; a block writes one row of partial sums, and a second kernel adds those up: fixed orders, the same bits each time.
+template <typename T, int C, bool BLOCK, bool VEC, bool TAN>
+__global__ void __launch_bounds__(BLOCK ? rownorm_block_threads<T>() : ROWNORM_BWD_THREADS, BLOCK ? 1 : 3)
+row_norm_bwd_kernel(const RowNormParams p) {
+    constexpr int V = RmsVec<T>::N, N = TAN ? 5 : 2;
+    __shared__ float slots[BLOCK ? 2 * 32 * N : 32 * ROWNORM_WARP_CHUNKS * V];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rpw = BLOCK ? 1 : 32 / p.P;
+    const RowLane<T, VEC> L{BLOCK ? (int)threadIdx.x : lane & (p.P - 1), BLOCK ? (int)blockDim.x : p.P, p.D};
+    const unsigned per_block = BLOCK ? 1u : (ROWNORM_BWD_THREADS / 32) * rpw;
+    const float inv_d = 1.0f / (float)p.D;
+    unsigned turn = 0;
+    uint64_t dg[C][V / 2];
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) dg[i][e] = 0ull;
+    for (unsigned base = blockIdx.x * per_block; base < p.total; base += gridDim.x * per_block) {
+        const unsigned row = BLOCK ? base : base + warp * rpw + lane / p.P;
+        const bool act = BLOCK || row < p.total;
+        const unsigned at = act ? row : 0;
+        uint4 hr[C], yr[C], tr[TAN ? C : 1], zr[TAN ? C : 1];   // as loaded: half the registers that bf16 rows would take as fp32
+        {
+            const T *ph = row_at<const T>(p.in[0], at, p), *py = row_at<const T>(p.in[1], at, p);
+#pragma unroll
+            for (int i = 0; i < C; ++i) { hr[i] = L.raw(ph, act, i); yr[i] = L.raw(py, act, i); }
+            if constexpr (TAN) {
+                const T *pt = row_at<const T>(p.in[3], at, p), *pz = row_at<const T>(p.in[4], at, p);
+#pragma unroll
+                for (int i = 0; i < C; ++i) { tr[i] = L.raw(pt, act, i); zr[i] = L.raw(pz, act, i); }
+            }
+        }
+        auto unpack = [&](int i, uint64_t (&h)[V / 2], uint64_t (&y)[V / 2], uint64_t (&t)[V / 2], uint64_t (&z)[V / 2]) {
+            rms_unpack(hr[i], h);
+            rms_unpack(yr[i], y);
+            if constexpr (TAN) { rms_unpack(tr[i], t); rms_unpack(zr[i], z); }
+        };
+        // Ends the reuse of an earlier unpacking across the reductions.
+        auto keep = [](uint4& q) { asm volatile("" : "+r"(q.x), "+r"(q.y), "+r"(q.z), "+r"(q.w)); };
+        // h.h, a.h, then with tangents h.th, b.h, b.th; h times `pre`
+        float s[N], pre = 1.f;
+        auto sum_up = [&]() {
+            const uint64_t pre2 = ptx::pack2(pre, pre);
+            uint64_t acc[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) acc[k] = 0ull;
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                uint64_t g[V / 2], h[V / 2], y[V / 2], t[V / 2], z[V / 2];
+                L.scale(p.g, i, g);
+                unpack(i, h, y, t, z);
+#pragma unroll
+                for (int e = 0; e < V / 2; ++e) {
+                    const uint64_t x = ptx::mul2(h[e], pre2);
+                    acc[0] = ptx::fma2(x, x, acc[0]);
+                    acc[1] = ptx::fma2(ptx::mul2(g[e], y[e]), x, acc[1]);
+                    if constexpr (TAN) {
+                        const uint64_t b = ptx::mul2(g[e], z[e]);
+                        acc[2] = ptx::fma2(x, t[e], acc[2]);
+                        acc[3] = ptx::fma2(b, x, acc[3]);
+                        acc[4] = ptx::fma2(b, t[e], acc[4]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < N; ++k) s[k] = rms_hsum(acc[k]);
+            row_reduce<N, false, BLOCK>(s, p.P, slots + (BLOCK ? (turn++ & 1u) * 32 * N : 0));
+        };
+        sum_up();
+        const float again = row_rescale(s[0], p.eps);
+        if (BLOCK ? again != 0.f : __any_sync(0xffffffffu, again != 0.f)) {
+            pre = again != 0.f ? again : 1.f;
+            sum_up();
+        }
+        const float root = 1.0f / sqrtf(s[0] * inv_d + p.eps * pre * pre), inv = root * pre;
+        const float au = s[1] * root;
+        // dx = inv a + kh u + kb b + kt th, dtx = inv b + zh u;  u = h inv
+        float kh = -inv * au * inv_d, kb = 0.f, kt = 0.f, zh = 0.f, jt = 0.f;
+        if constexpr (TAN) {
+            const float ut = s[2] * root, bu = s[3] * root, f = inv * inv * inv_d;
+            kh += f * (3.f * bu * ut * inv_d - s[4]);
+            kb = -f * ut;
+            kt = -f * bu;
+            zh = -inv * bu * inv_d;
+            jt = -inv * ut * inv_d;
+        }
+        if (act) {
+            const uint64_t inv2 = ptx::pack2(inv, inv), kh2 = ptx::pack2(kh, kh), kb2 = ptx::pack2(kb, kb), kt2 = ptx::pack2(kt, kt);
+            const uint64_t zh2 = ptx::pack2(zh, zh), jt2 = ptx::pack2(jt, jt);
+            T* dx = row_at<T>(p.out[0], at, p);
+            T* dtx = TAN ? row_at<T>(p.out[1], at, p) : nullptr;
+            const T* dh = p.in[2].p ? row_at<const T>(p.in[2], at, p) : nullptr;
+            const T* dth = TAN && p.in[5].p ? row_at<const T>(p.in[5], at, p) : nullptr;
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                uint64_t g[V / 2], ox[V / 2], ot[V / 2], h[V / 2], y[V / 2], t[V / 2], z[V / 2];
+#pragma unroll
+                for (int e = 0; e < V / 2; ++e) ox[e] = ot[e] = 0ull;
+                if (dh) L.load(dh, true, i, ox);
+                if (dth) L.load(dth, true, i, ot);
+                L.scale(p.g, i, g);
+                keep(hr[i]); keep(yr[i]);
+                if constexpr (TAN) { keep(tr[i]); keep(zr[i]); }
+                unpack(i, h, y, t, z);
+#pragma unroll
+                for (int e = 0; e < V / 2; ++e) {
+                    const uint64_t u = ptx::mul2(h[e], inv2), a = ptx::mul2(g[e], y[e]);
+                    ox[e] = ptx::add2(ptx::fma2(a, inv2, ptx::mul2(u, kh2)), ox[e]);
+                    uint64_t term = ptx::mul2(y[e], u);
+                    if constexpr (TAN) {
+                        const uint64_t b = ptx::mul2(g[e], z[e]);
+                        ox[e] = ptx::fma2(b, kb2, ptx::fma2(t[e], kt2, ox[e]));
+                        ot[e] = ptx::add2(ptx::fma2(b, inv2, ptx::mul2(u, zh2)), ot[e]);
+                        term = ptx::fma2(z[e], ptx::fma2(t[e], inv2, ptx::mul2(u, jt2)), term);
+                    }
+                    dg[i][e] = ptx::add2(dg[i][e], term);
+                }
+                L.store(dx, i, ox);
+                if constexpr (TAN) L.store(dtx, i, ot);
+            }
+        }
+    }
+    if (!p.aux) return;
+    // the reduction may be launched: its blocks wait for this grid's end before they read anything
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    float* partial = p.aux + (size_t)blockIdx.x * p.D;
+    if constexpr (BLOCK) {
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float a, b;
+                ptx::unpack2(dg[i][e / 2], a, b);
+                if (L.col(i, e) < p.D) partial[L.col(i, e)] = e & 1 ? b : a;
+            }
+    } else {
+        for (int w = 0; w < ROWNORM_BWD_THREADS / 32; ++w) {   // the warps one after the other
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    float a, b;
+                    ptx::unpack2(dg[i][e / 2], a, b);
+                    float v = e & 1 ? b : a;
+                    if (warp == w) {
+                        for (int off = 16; off >= p.P; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);   // the rows of a warp
+                        if (lane < p.P && L.col(i, e) < p.D) slots[L.col(i, e)] = w == 0 ? v : slots[L.col(i, e)] + v;
+                    }
+                }
+        }
+        __syncthreads();
+        for (int j = threadIdx.x; j < p.D; j += ROWNORM_BWD_THREADS) partial[j] = slots[j];
+    }
+}
+
+// dg[j] = sum over the n partial rows, in a fixed order: a warp takes every 32nd row of 32 columns.  Launched as a programmatic
+// dependent of the kernel above.  n = 0 (no rows at all) gives zeros.
+__global__ void __launch_bounds__(1024) row_norm_dg_kernel(const float* __restrict__ partial, float* __restrict__ dg, int n, int D) {
+    __shared__ float acc[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    float v = 0.f;
+    if (j < D) {
+#pragma unroll 8
+        for (int b = warp; b < n; b += 32) v += partial[(size_t)b * D + j];
+    }
+    acc[warp][lane] = v;
+    __syncthreads();
+    v = acc[lane][warp];   // column `warp` of the 32, partial sum `lane`
+    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    if (lane == 0 && blockIdx.x * 32 + warp < D) dg[blockIdx.x * 32 + warp] = v;
+}
+
+}  // namespace tvm_attn

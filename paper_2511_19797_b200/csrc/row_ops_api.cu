@@ -1,0 +1,291 @@
+// C-ABI entry points of the operators on rows of the model width (see include/tvm_attn.h): the RMSNorm with residual and
+// tangent, its backward and its 8-bit form, and the products of 8-bit rows.  Argument checks and launches.
+#include "tvm_attn.h"
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstring>
+#include <type_traits>
+
+#include "host_common.h"
+#include "linear_s8.cuh"
+#include "row_norm.cuh"
+
+namespace tvm_attn {
+
+// ------------------------------------------------------------------------------------------------ rows
+static int check_rows_params(const tvm_attn_rows_params* p) {
+    if (!p || p->B < 0 || p->T < 0 || p->D <= 0) return TVM_ATTN_INVALID_ARG;
+    if (p->dtype != TVM_ATTN_BF16 && p->dtype != TVM_ATTN_FP32) return TVM_ATTN_INVALID_ARG;
+    if (!(p->eps >= 0.0f) || !std::isfinite(p->eps)) return TVM_ATTN_INVALID_ARG;
+    if (p->D > TVM_ATTN_MAX_WIDTH || (long long)p->B * p->T > 2147483647LL) return TVM_ATTN_UNSUPPORTED;
+    return TVM_ATTN_OK;
+}
+
+static bool present(const tvm_attn_rows* t) { return t && t->ptr; }
+
+// What the tensors of a call have in common, gathered while they are checked.
+struct RowsCall {
+    const tvm_attn_rows_params& p;
+    RowNormParams k;
+    bool vec;   // every row begins on 16 bytes (8-bit rows: 8) and is a multiple of 16 bytes long
+    int esz;
+    bool ok = true;
+    explicit RowsCall(const tvm_attn_rows_params& q) : p(q) {
+        std::memset(&k, 0, sizeof k);
+        esz = q.dtype == TVM_ATTN_FP32 ? 4 : 2;
+        k.total = (unsigned)((long long)q.B * q.T);
+        k.T = k.total;   // one dimension of rows, until a tensor needs two
+        k.D = q.D;
+        k.eps = q.eps;
+        vec = q.D * esz % 16 == 0;
+    }
+    void add(const tvm_attn_rows* t, RowsPtr* to, bool required, bool eight = false) {
+        if (!present(t)) {
+            ok = ok && !required;
+            return;
+        }
+        const long long size = eight ? 1 : esz;
+        long long row = t->row, batch = t->batch;
+        if (row == 0 && batch == 0) { row = p.D; batch = (long long)p.T * p.D; }
+        if (p.T <= 1) row = batch;          // one row a batch: the batches are the rows
+        if (p.B <= 1) batch = row * p.T;
+        if (k.total <= 1) row = batch = p.D;
+        if (row < p.D || batch < p.D || row > (1LL << 40) || batch > (1LL << 40) || reinterpret_cast<uintptr_t>(t->ptr) % size) { ok = false; return; }
+        *to = {t->ptr, row, batch};
+        if (p.T > 1 && batch != row * p.T) k.T = (unsigned)p.T;
+        const long long unit = eight ? 8 : 16;
+        vec = vec && reinterpret_cast<uintptr_t>(t->ptr) % unit == 0 && row * size % unit == 0 && batch * size % unit == 0;
+    }
+    void scale(const float* g) {
+        k.g = g;
+        ok = ok && reinterpret_cast<uintptr_t>(g) % 4 == 0;
+        vec = vec && aligned16(g);   // (a null scale is aligned)
+    }
+};
+
+// How a row is split over threads: chunks of 16 bytes, C on each of P lanes of a warp, or of a block of `threads`.
+struct RowSplit { int C, P, threads; };
+static RowSplit row_split(int D, int esz) {
+    const int chunks = (D * esz + 15) / 16;
+    if (chunks <= 32 * ROWNORM_WARP_CHUNKS) {
+        // four chunks on as few lanes as that takes (a warp has more rows, and fewer steps to add one up)
+        int P = 1;
+        while (P < 32 && 4 * P < chunks) P *= 2;
+        const int C = (chunks + P - 1) / P;
+        return {C < 2 ? 2 : C, P, 0};
+    }
+    const int warps = (chunks + 127) / 128;   // three or four chunks a thread
+    return {(chunks + 32 * warps - 1) / (32 * warps), 32 * warps, 32 * warps};
+}
+
+// launch(C, whether a row has a block) as types, for the split of a call.
+template <typename F>
+static int with_row_split(const RowSplit& s, const F& launch) {
+    using std::integral_constant;
+    if (s.threads) return s.C <= 3 ? launch(integral_constant<int, 3>(), std::true_type()) : launch(integral_constant<int, 4>(), std::true_type());
+    switch (s.C) {
+        case 2: return launch(integral_constant<int, 2>(), std::false_type());
+        case 3: return launch(integral_constant<int, 3>(), std::false_type());
+        case 4: return launch(integral_constant<int, 4>(), std::false_type());
+        default: return launch(integral_constant<int, 5>(), std::false_type());
+    }
+}
+
+static unsigned fewer(long long a, long long b) { return (unsigned)(a < b ? a : b); }
+
+template <typename T, int MODE>
+static int launch_norm(const RowsCall& c, cudaStream_t st) {
+    const RowSplit split = row_split(c.k.D, sizeof(T));
+    RowNormParams k = c.k;
+    k.P = split.P;
+    return with_row_split(split, [&](auto C, auto block) {
+        // more blocks than an SM holds at a time: a block that has stored its rows leaves room for one that loads
+        const int per_block = block() ? 1 : ROWNORM_THREADS / 32 * (32 / k.P), threads = block() ? split.threads : ROWNORM_THREADS;
+        const unsigned grid = fewer((k.total + (long long)per_block - 1) / per_block, 148LL * 64);
+        if (c.vec) row_norm_kernel<T, C(), block(), true, MODE><<<grid, threads, 0, st>>>(k);
+        else row_norm_kernel<T, C(), block(), false, MODE><<<grid, threads, 0, st>>>(k);
+        g_launches += 1;
+        return cuda_status(cudaGetLastError());
+    });
+}
+
+template <int MODE>
+static int launch_norm(const RowsCall& c, cudaStream_t st) {
+    return c.p.dtype == TVM_ATTN_FP32 ? launch_norm<float, MODE>(c, st) : launch_norm<__nv_bfloat16, MODE>(c, st);
+}
+
+static int bwd_blocks(const RowSplit& split, long long rows) {
+    const int per_block = split.threads ? 1 : ROWNORM_BWD_THREADS / 32 * (32 / split.P);
+    return (int)fewer((rows + per_block - 1) / per_block, rownorm_bwd_blocks(split.threads / 32));
+}
+
+template <typename T, bool TAN>
+static int launch_norm_bwd(const RowsCall& c, float* dg, cudaStream_t st) {
+    const RowSplit split = row_split(c.k.D, sizeof(T));
+    RowNormParams k = c.k;
+    k.P = split.P;
+    const int blocks = bwd_blocks(split, k.total);
+    if (blocks > 0) {
+        const int rc = with_row_split(split, [&](auto C, auto block) {
+            const int threads = block() ? split.threads : ROWNORM_BWD_THREADS;
+            if (c.vec) row_norm_bwd_kernel<T, C(), block(), true, TAN><<<blocks, threads, 0, st>>>(k);
+            else row_norm_bwd_kernel<T, C(), block(), false, TAN><<<blocks, threads, 0, st>>>(k);
+            g_launches += 1;
+            return cuda_status(cudaGetLastError());
+        });
+        if (rc != TVM_ATTN_OK) return rc;
+    }
+    if (!dg) return TVM_ATTN_OK;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(k.D + 31) / 32);
+    cfg.blockDim = dim3(1024);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = blocks > 0 ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, row_norm_dg_kernel, (const float*)k.aux, dg, blocks, k.D);
+    if (e == cudaSuccess) g_launches += 1;
+    else cudaGetLastError();
+    return cuda_status(e);
+}
+
+static size_t norm_bwd_workspace(const tvm_attn_rows_params& p) {
+    const RowSplit split = row_split(p.D, p.dtype == TVM_ATTN_FP32 ? 4 : 2);
+    return (size_t)rownorm_bwd_blocks(split.threads / 32) * (size_t)p.D * sizeof(float);
+}
+
+}  // namespace tvm_attn
+
+using namespace tvm_attn;
+
+extern "C" {
+
+int tvm_attn_rmsnorm_jvp_fwd(const tvm_attn_rows_params* p, const tvm_attn_rows* x, const tvm_attn_rows* res, const tvm_attn_rows* tx,
+                             const tvm_attn_rows* tres, const float* g, const tvm_attn_rows* y, const tvm_attn_rows* h,
+                             const tvm_attn_rows* ty, const tvm_attn_rows* th, void* cuda_stream) {
+    const int rc = check_rows_params(p);
+    if (rc != TVM_ATTN_OK) return rc;
+    if (present(res) != present(h) || present(tx) != present(ty) || present(tres) != present(th) || (present(tres) && !present(tx))) return TVM_ATTN_INVALID_ARG;
+    RowsCall c(*p);
+    if (c.k.total == 0) return TVM_ATTN_OK;
+    c.add(x, &c.k.in[0], true); c.add(res, &c.k.in[1], false); c.add(tx, &c.k.in[2], false); c.add(tres, &c.k.in[3], false);
+    c.add(y, &c.k.out[0], true); c.add(h, &c.k.out[1], false); c.add(ty, &c.k.out[2], false); c.add(th, &c.k.out[3], false);
+    c.scale(g);
+    if (!c.ok) return TVM_ATTN_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    return present(tx) ? launch_norm<ROW_NORM_TAN>(c, st) : launch_norm<ROW_NORM>(c, st);
+}
+
+size_t tvm_attn_rmsnorm_jvp_workspace_bytes(const tvm_attn_rows_params* p) {
+    return check_rows_params(p) == TVM_ATTN_OK ? norm_bwd_workspace(*p) : 0;
+}
+
+int tvm_attn_rmsnorm_jvp_bwd(const tvm_attn_rows_params* p, const tvm_attn_rows* h, const tvm_attn_rows* dy, const tvm_attn_rows* dh,
+                             const tvm_attn_rows* th, const tvm_attn_rows* dty, const tvm_attn_rows* dth, const float* g,
+                             const tvm_attn_rows* dx, const tvm_attn_rows* dtx, float* dg, void* workspace, size_t workspace_bytes,
+                             void* cuda_stream) {
+    const int rc = check_rows_params(p);
+    if (rc != TVM_ATTN_OK) return rc;
+    if (present(th) != present(dty) || present(th) != present(dtx) || (present(dth) && !present(th)) || !g != !dg) return TVM_ATTN_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(dg) % 4) return TVM_ATTN_INVALID_ARG;
+    RowsCall c(*p);
+    c.scale(g);
+    if (c.k.total > 0) {
+        c.add(h, &c.k.in[0], true); c.add(dy, &c.k.in[1], true); c.add(dh, &c.k.in[2], false);
+        c.add(th, &c.k.in[3], false); c.add(dty, &c.k.in[4], false); c.add(dth, &c.k.in[5], false);
+        c.add(dx, &c.k.out[0], true); c.add(dtx, &c.k.out[1], false);
+    }
+    if (!c.ok) return TVM_ATTN_INVALID_ARG;
+    if (g) {
+        if (!workspace || !aligned16(workspace)) return TVM_ATTN_INVALID_ARG;
+        if (workspace_bytes < norm_bwd_workspace(*p)) return TVM_ATTN_WORKSPACE_TOO_SMALL;
+        c.k.aux = static_cast<float*>(workspace);
+    }
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (p->dtype == TVM_ATTN_FP32) return present(th) ? launch_norm_bwd<float, true>(c, dg, st) : launch_norm_bwd<float, false>(c, dg, st);
+    return present(th) ? launch_norm_bwd<__nv_bfloat16, true>(c, dg, st) : launch_norm_bwd<__nv_bfloat16, false>(c, dg, st);
+}
+
+int tvm_attn_rmsnorm_s8(const tvm_attn_rows_params* p, const tvm_attn_rows* x, const tvm_attn_rows* res, const float* g,
+                        const tvm_attn_rows* q, float* s, const tvm_attn_rows* h, void* cuda_stream) {
+    const int rc = check_rows_params(p);
+    if (rc != TVM_ATTN_OK) return rc;
+    if (present(res) != present(h)) return TVM_ATTN_INVALID_ARG;
+    RowsCall c(*p);
+    if (c.k.total == 0) return TVM_ATTN_OK;
+    c.add(x, &c.k.in[0], true); c.add(res, &c.k.in[1], false);
+    c.add(q, &c.k.out[0], true, true); c.add(h, &c.k.out[1], false);
+    c.scale(g);
+    if (!c.ok || !s || reinterpret_cast<uintptr_t>(s) % 4) return TVM_ATTN_INVALID_ARG;
+    c.k.aux = s;
+    c.k.norm = true;
+    return launch_norm<ROW_S8>(c, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int tvm_attn_quantize_s8(const tvm_attn_rows_params* p, const tvm_attn_rows* x, const tvm_attn_rows* q, float* s, void* cuda_stream) {
+    const int rc = check_rows_params(p);
+    if (rc != TVM_ATTN_OK) return rc;
+    RowsCall c(*p);
+    if (c.k.total == 0) return TVM_ATTN_OK;
+    c.add(x, &c.k.in[0], true);
+    c.add(q, &c.k.out[0], true, true);
+    if (!c.ok || !s || reinterpret_cast<uintptr_t>(s) % 4) return TVM_ATTN_INVALID_ARG;
+    c.k.aux = s;
+    c.k.eps = 1.f;   // (the sum of squares is not used: nothing is to be scaled for it)
+    return launch_norm<ROW_S8>(c, static_cast<cudaStream_t>(cuda_stream));
+}
+
+}  // extern "C"
+
+namespace tvm_attn {
+
+// ------------------------------------------------------------------------------------------------ 8-bit products
+template <typename OUT, int NT>
+static int launch_few(const LinearParams& p, cudaStream_t st) {
+    const int rows = 16 * (LIN_FEW_THREADS / 32 / p.ksplit);
+    const dim3 grid((unsigned)((p.N + rows - 1) / rows), (unsigned)((p.M + 8 * NT - 1) / (8 * NT)));
+    linear_s8_few_kernel<OUT, NT><<<grid, LIN_FEW_THREADS, 0, st>>>(p);
+    g_launches += 1;
+    return cuda_status(cudaGetLastError());
+}
+
+template <typename OUT>
+static int linear_few(LinearParams p, cudaStream_t st) {
+    // warps of a block that share k: until there are some 16 warps for every SM, or 256 bytes of k for each
+    const long long groups = (p.N + 15) / 16;
+    p.ksplit = 1;
+    while (p.ksplit < 8 && groups * p.ksplit < 148 * 16 && p.K > 64 * LIN_FEW_UNROLL * p.ksplit) p.ksplit *= 2;
+    if (p.M <= 8) return launch_few<OUT, 1>(p, st);
+    if (p.M <= 16) return launch_few<OUT, 2>(p, st);
+    if (p.M <= 32) return launch_few<OUT, 4>(p, st);
+    return launch_few<OUT, 8>(p, st);
+}
+
+}  // namespace tvm_attn
+
+extern "C" int tvm_attn_linear_s8(const tvm_attn_linear_params* p, const void* q, const float* s, const void* w, const float* ws, const float* bias,
+                                  void* y, void* cuda_stream) {
+    if (!p || p->M < 0 || p->N <= 0 || p->K <= 0) return TVM_ATTN_INVALID_ARG;
+    if (p->dtype != TVM_ATTN_BF16 && p->dtype != TVM_ATTN_FP32) return TVM_ATTN_INVALID_ARG;
+    const long long ldq = p->ldq ? p->ldq : p->K, ldw = p->ldw ? p->ldw : p->K, ldy = p->ldy ? p->ldy : p->N;
+    if (ldq < p->K || ldw < p->K || ldy < p->N || ldq % 16 || ldw % 16) return TVM_ATTN_INVALID_ARG;
+    // sums of K products of at most 2^14 in 32 bits; strides as a tensor map holds them
+    if (p->K > 65536 || ldq >= (1LL << 38) || ldw >= (1LL << 38) || ldy >= (1LL << 36)) return TVM_ATTN_UNSUPPORTED;
+    if (p->M == 0) return TVM_ATTN_OK;
+    const int esz = p->dtype == TVM_ATTN_FP32 ? 4 : 2;
+    if (!q || !s || !w || !ws || !y || !aligned16(q) || !aligned16(w) || reinterpret_cast<uintptr_t>(y) % esz) return TVM_ATTN_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(s) % 4 || reinterpret_cast<uintptr_t>(ws) % 4 || reinterpret_cast<uintptr_t>(bias) % 4) return TVM_ATTN_INVALID_ARG;
+    LinearParams k;
+    std::memset(&k, 0, sizeof k);
+    k.q = static_cast<const int8_t*>(q); k.w = static_cast<const int8_t*>(w);
+    k.s = s; k.ws = ws; k.bias = bias; k.y = y;
+    k.ldq = ldq; k.ldw = ldw; k.ldy = ldy;
+    k.M = p->M; k.N = p->N; k.K = p->K;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    return p->dtype == TVM_ATTN_FP32 ? linear_few<float>(k, st) : linear_few<__nv_bfloat16>(k, st);
+}

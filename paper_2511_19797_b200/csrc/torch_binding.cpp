@@ -23,6 +23,7 @@
 
 #include <cstring>
 #include <stdexcept>
+#include <vector>
 
 #include "tvm_attn.h"
 
@@ -35,6 +36,12 @@ decltype(&tvm_attn_jvp_workspace_bytes) p_ws = nullptr;
 decltype(&tvm_qk_rmsnorm_jvp_fwd) p_norm_fwd = nullptr;
 decltype(&tvm_qk_rmsnorm_jvp_bwd) p_norm_bwd = nullptr;
 decltype(&tvm_qk_rmsnorm_jvp_workspace_bytes) p_norm_ws = nullptr;
+decltype(&tvm_attn_rmsnorm_jvp_fwd) p_rows_fwd = nullptr;
+decltype(&tvm_attn_rmsnorm_jvp_bwd) p_rows_bwd = nullptr;
+decltype(&tvm_attn_rmsnorm_jvp_workspace_bytes) p_rows_ws = nullptr;
+decltype(&tvm_attn_rmsnorm_s8) p_rows_s8 = nullptr;
+decltype(&tvm_attn_quantize_s8) p_quantize = nullptr;
+decltype(&tvm_attn_linear_s8) p_linear = nullptr;
 
 struct ValueError : std::runtime_error { using std::runtime_error::runtime_error; };
 
@@ -105,17 +112,18 @@ void used_on(const at::Tensor* ts, int n, PyObject* callers, c10::cuda::CUDAStre
         if (ts[i].defined()) c10::cuda::CUDACachingAllocator::recordStream(ts[i].storage().data_ptr(), st);
 }
 
+PyObject* same(PyObject* o) { Py_INCREF(o); return o; }
+// Undefined tensors come out as None.
 PyObject* tuple_of(at::Tensor* ts, int n) {
     PyObject* r = PyTuple_New(n);
     if (!r) return nullptr;
     for (int i = 0; i < n; ++i) {
-        PyObject* o = THPVariable_Wrap(std::move(ts[i]));
+        PyObject* o = ts[i].defined() ? THPVariable_Wrap(std::move(ts[i])) : same(Py_None);
         if (!o) { Py_DECREF(r); return nullptr; }
         PyTuple_SET_ITEM(r, i, o);
     }
     return r;
 }
-PyObject* same(PyObject* o) { Py_INCREF(o); return o; }
 
 template <typename F>
 PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F&& f) {
@@ -294,11 +302,249 @@ PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// bind(addresses of tvm_attn_jvp_fwd, _bwd, _bwd_noalloc, _workspace_bytes, tvm_qk_rmsnorm_jvp_fwd, _bwd, _workspace_bytes)
+// ------------------------------------------------------------------------------------------------ rows of the model width
+// The tensors (..., D) of a call as (B, T, D): leading dimensions of one element drop out, and two merge where they do in every
+// tensor of the call.
+struct Rows {
+    static constexpr int MOST = 10;
+    const at::Tensor* ts[MOST];
+    tvm_attn_rows at[MOST];
+    int n = 0;
+    tvm_attn_rows_params p;
+
+    // The place of a tensor's tvm_attn_rows, a null pointer for an absent tensor.  `eight`: 8-bit rows.
+    tvm_attn_rows* add(const at::Tensor& t, bool eight = false) {
+        if (!t.defined()) return nullptr;
+        const at::Tensor& ref = n ? *ts[0] : t;
+        if (t.sizes() != ref.sizes() || t.device() != ref.device() || t.scalar_type() != (eight ? at::kChar : ref.scalar_type()))
+            throw ValueError("the tensors of a call must share shape, dtype and device (8-bit rows: int8)");
+        if (!t.is_cuda()) throw ValueError("tensors must be CUDA tensors");
+        if (t.dim() < 1) throw ValueError("expected (..., D) tensors");
+        if (t.stride(-1) != 1 && t.size(-1) != 1 && t.numel() > 0) throw ValueError("the D elements of a row must be contiguous");
+        ts[n] = &t;
+        return &at[n++];
+    }
+    void merge(double eps) {
+        const at::Tensor& ref = *ts[0];
+        std::memset(&p, 0, sizeof p);
+        if (ref.scalar_type() == at::kBFloat16) p.dtype = TVM_ATTN_BF16;
+        else if (ref.scalar_type() == at::kFloat) p.dtype = TVM_ATTN_FP32;
+        else throw ValueError("tensors must be bfloat16 or float32");
+        const int64_t D = ref.size(-1);
+        if (D < 1 || D > INT32_MAX) throw ValueError("rows must have one element or more");
+        int64_t count[2] = {1, 1}, stride[MOST][2] = {};
+        int groups = 0;
+        if (ref.numel() == 0) count[0] = 0;
+        else
+            for (int64_t d = ref.dim() - 2; d >= 0; --d) {
+                if (ref.size(d) == 1) continue;
+                bool merges = groups > 0;
+                for (int i = 0; i < n && merges; ++i) merges = ts[i]->stride(d) == stride[i][groups - 1] * count[groups - 1];
+                if (merges) { count[groups - 1] *= ref.size(d); continue; }
+                if (groups == 2) throw ValueError("the rows of a call's tensors must lie in at most two strides");
+                for (int i = 0; i < n; ++i) stride[i][groups] = ts[i]->stride(d);
+                count[groups++] = ref.size(d);
+            }
+        if (count[0] > INT32_MAX || count[1] > INT32_MAX) throw ValueError("dimensions must fit 32 bits");
+        p.T = (int32_t)count[0]; p.B = (int32_t)count[1]; p.D = (int32_t)D;
+        p.eps = (float)eps;
+        for (int i = 0; i < n; ++i) {
+            if (groups < 1) stride[i][0] = D;
+            if (groups < 2) stride[i][1] = stride[i][0] * (count[0] ? count[0] : 1);
+            if (stride[i][0] < D || stride[i][1] < D) throw ValueError("the rows of a tensor must not overlap");
+            at[i] = {ts[i]->data_ptr(), stride[i][0], stride[i][1]};
+        }
+    }
+};
+
+// A new packed tensor with the shape of t.
+at::Tensor packed_like(const at::Tensor& t) { return packed(t.sizes(), t.scalar_type(), t.device()); }
+// New 8-bit rows with the shape of t: rows begin on 16 bytes.
+at::Tensor rows8(const at::Tensor& t) {
+    const int64_t dims = t.dim(), D = t.size(-1);
+    std::vector<int64_t> st(dims);
+    st[dims - 1] = 1;
+    int64_t step = (D + 15) / 16 * 16;
+    for (int64_t d = dims - 2; d >= 0; --d) { st[d] = step; step *= t.size(d) > 0 ? t.size(d) : 1; }
+    return at::Tensor(at::detail::empty_strided_cuda(t.sizes(), st, at::kChar, t.device()));
+}
+void check_vector(const at::Tensor& v, int64_t n, const at::Device& dev, const char* what) {
+    if (!v.defined()) return;
+    if (v.scalar_type() != at::kFloat || v.dim() != 1 || v.numel() != n || v.device() != dev || !v.is_contiguous()) throw ValueError(what);
+}
+void check_scales(const at::Tensor& s, const at::Tensor& rows) {
+    if (s.scalar_type() != at::kFloat || s.sizes() != rows.sizes().slice(0, rows.dim() - 1) || s.device() != rows.device() || !s.is_contiguous())
+        throw ValueError("the scales of 8-bit rows must be contiguous float32, one for each row");
+}
+// The outputs of a call: given ones, of which there is one exactly where one is computed, or new ones.
+void outputs(bool given, at::Tensor* o, const bool* wanted, const at::Tensor& like, int n) {
+    for (int i = 0; i < n; ++i) {
+        if (given) {
+            if (o[i].defined() != wanted[i]) throw ValueError("`out` must hold a tensor for each output that the call computes, and None for the others");
+        } else if (wanted[i]) {
+            o[i] = packed_like(like);
+        }
+    }
+}
+constexpr const char* kScaleText = "the scale must be a contiguous float32 CUDA vector of D elements";
+
+// rows_fwd(x, res | None, tx | None, tres | None, g | None, eps, out | None, stream | None) -> (y, h, ty, th)
+PyObject* rows_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 8, [&]() -> PyObject* {
+        const at::Tensor& x = tensor(a[0]);
+        const at::Tensor res = optional_tensor(a[1]), tx = optional_tensor(a[2]), tres = optional_tensor(a[3]), g = optional_tensor(a[4]);
+        if (tres.defined() && !tx.defined()) throw ValueError("a residual's tangent needs the tangent that it is added to");
+        Rows r;
+        const auto *rx = r.add(x), *rres = r.add(res), *rtx = r.add(tx), *rtres = r.add(tres);
+        check_vector(g, x.size(-1), x.device(), kScaleText);
+        at::Tensor o[4];
+        const bool given = a[6] != Py_None, wanted[4] = {true, res.defined(), tx.defined(), tres.defined()};
+        const c10::cuda::CUDAGuard guard(x.device());
+        if (given) entries(a[6], 4, o, false);
+        outputs(given, o, wanted, x, 4);
+        const auto *ry = r.add(o[0]), *rh = r.add(o[1]), *rty = r.add(o[2]), *rth = r.add(o[3]);
+        r.merge(number(a[5]));
+        const c10::cuda::CUDAStream st = stream_of(a[7], x.device());
+        if (!given) used_on(o, 4, a[7], st);
+        const int rc = without_gil([&] { return p_rows_fwd(&r.p, rx, rres, rtx, rtres, (float*)ptr(g), ry, rh, rty, rth, st.stream()); });
+        if (rc != TVM_ATTN_OK) return PyLong_FromLong(rc);
+        if (!res.defined()) o[1] = x;
+        if (!tres.defined()) o[3] = tx;
+        return tuple_of(o, 4);
+    });
+}
+
+// rows_bwd(h, dy, th | None, dty | None, dh | None, dth | None, g | None, eps, out | None, workspace | None, stream | None) -> (dx, dtx, dg)
+PyObject* rows_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 11, [&]() -> PyObject* {
+        const at::Tensor &h = tensor(a[0]), &dy = tensor(a[1]);
+        const at::Tensor th = optional_tensor(a[2]), dty = optional_tensor(a[3]), dh = optional_tensor(a[4]), dth = optional_tensor(a[5]), g = optional_tensor(a[6]);
+        if (th.defined() != dty.defined()) throw ValueError("the tangent and the cotangent of the norm's tangent come together");
+        if (dth.defined() && !th.defined()) throw ValueError("a cotangent of the tangent needs the tangent");
+        Rows r;
+        const auto *rh = r.add(h), *rdy = r.add(dy), *rdh = r.add(dh), *rth = r.add(th), *rdty = r.add(dty), *rdth = r.add(dth);
+        check_vector(g, h.size(-1), h.device(), kScaleText);
+        at::Tensor o[3];
+        const bool given = a[8] != Py_None, wanted[2] = {true, th.defined()};
+        const c10::cuda::CUDAGuard guard(h.device());
+        if (given) entries(a[8], 3, o, false);
+        outputs(given, o, wanted, h, 2);
+        if (!given && g.defined()) o[2] = packed_like(g);
+        if (o[2].defined() != g.defined()) throw ValueError("`out` must hold a tensor for each output that the call computes, and None for the others");
+        check_vector(o[2], h.size(-1), h.device(), kScaleText);
+        const auto *rdx = r.add(o[0]), *rdtx = r.add(o[1]);
+        r.merge(number(a[7]));
+        at::Tensor ws = optional_tensor(a[9]);
+        const bool own_ws = !ws.defined() && g.defined();
+        if (own_ws) ws = packed({(int64_t)p_rows_ws(&r.p) + 16}, at::kByte, h.device());
+        if (ws.defined() && (ws.device() != h.device() || !ws.is_contiguous())) throw ValueError("the workspace must be contiguous and on the tensors' device");
+        const c10::cuda::CUDAStream st = stream_of(a[10], h.device());
+        if (!given) used_on(o, 3, a[10], st);
+        if (own_ws) used_on(&ws, 1, a[10], st);
+        const int rc = without_gil([&] {
+            return p_rows_bwd(&r.p, rh, rdy, rdh, rth, rdty, rdth, (float*)ptr(g), rdx, rdtx, (float*)ptr(o[2]), ptr(ws),
+                              ws.defined() ? (size_t)ws.nbytes() : 0, st.stream());
+        });
+        return rc != TVM_ATTN_OK ? PyLong_FromLong(rc) : tuple_of(o, 3);
+    });
+}
+
+// rows_s8(x, res | None, g | None, eps, norm, out | None, stream | None) -> (q, s, h) with norm, (q, s) without
+PyObject* rows_s8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 7, [&]() -> PyObject* {
+        const at::Tensor& x = tensor(a[0]);
+        const at::Tensor res = optional_tensor(a[1]), g = optional_tensor(a[2]);
+        const bool norm = a[4] == Py_True, given = a[5] != Py_None;
+        const int count = norm ? 3 : 2;
+        Rows r;
+        const auto *rx = r.add(x), *rres = r.add(res);
+        check_vector(g, x.size(-1), x.device(), kScaleText);
+        at::Tensor o[3];
+        const c10::cuda::CUDAGuard guard(x.device());
+        if (given) {
+            entries(a[5], count, o, false);
+            if (!o[0].defined() || !o[1].defined() || o[2].defined() != res.defined())
+                throw ValueError("`out` must hold a tensor for each output that the call computes, and None for the others");
+        } else {
+            o[0] = rows8(x);
+            o[1] = packed(x.sizes().slice(0, x.dim() - 1), at::kFloat, x.device());
+            if (res.defined()) o[2] = packed_like(x);
+        }
+        const auto *rq = r.add(o[0], true), *rh = r.add(o[2]);
+        check_scales(o[1], x);
+        r.merge(number(a[3]));
+        const c10::cuda::CUDAStream st = stream_of(a[6], x.device());
+        if (!given) used_on(o, 3, a[6], st);
+        const int rc = without_gil([&] {
+            return norm ? p_rows_s8(&r.p, rx, rres, (float*)ptr(g), rq, (float*)ptr(o[1]), rh, st.stream()) : p_quantize(&r.p, rx, rq, (float*)ptr(o[1]), st.stream());
+        });
+        if (rc != TVM_ATTN_OK) return PyLong_FromLong(rc);
+        if (!res.defined()) o[2] = x;
+        return tuple_of(o, count);
+    });
+}
+
+// The leading dimensions of t as one: their number of rows, and the elements between them (`least` where there are fewer than two).
+int64_t one_stride(const at::Tensor& t, int64_t least, int64_t* rows) {
+    if (t.stride(-1) != 1 && t.size(-1) != 1 && t.numel() > 0) throw ValueError("the elements of a row must be contiguous");
+    int64_t count = 1, stride = least;
+    if (t.numel() == 0) { *rows = 0; return least; }
+    for (int64_t d = t.dim() - 2; d >= 0; --d) {
+        if (t.size(d) == 1) continue;
+        if (count == 1) stride = t.stride(d);
+        else if (t.stride(d) != stride * count) throw ValueError("the rows of a product's tensors must lie in one stride");
+        count *= t.size(d);
+    }
+    if (count > 1 && stride < t.size(-1)) throw ValueError("the rows of a tensor must not overlap");
+    *rows = count;
+    return stride;
+}
+
+// linear_s8(q, s, w, ws, bias | None, fp32, out | None, stream | None) -> y
+PyObject* linear_s8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 8, [&]() -> PyObject* {
+        const at::Tensor &q = tensor(a[0]), &s = tensor(a[1]), &w = tensor(a[2]), &ws = tensor(a[3]);
+        const at::Tensor bias = optional_tensor(a[4]);
+        const at::ScalarType type = a[5] == Py_True ? at::kFloat : at::kBFloat16;
+        if (q.scalar_type() != at::kChar || w.scalar_type() != at::kChar || q.dim() < 1 || w.dim() != 2 || q.size(-1) != w.size(1) || q.device() != w.device())
+            throw ValueError("expected int8 rows (..., K) and int8 weights (N, K) on one device");
+        if (!q.is_cuda()) throw ValueError("tensors must be CUDA tensors");
+        const int64_t K = w.size(1), N = w.size(0);
+        if (K < 1 || N < 1 || K > INT32_MAX || N > INT32_MAX) throw ValueError("weights must have one row and one column or more");
+        check_scales(s, q);
+        check_vector(ws, N, q.device(), "the weights' scales must be a contiguous float32 vector of N elements");
+        check_vector(bias, N, q.device(), "the bias must be a contiguous float32 vector of N elements");
+        tvm_attn_linear_params p;
+        std::memset(&p, 0, sizeof p);
+        int64_t M, N_rows, M_out;
+        const int64_t pitch = (K + 15) / 16 * 16;
+        p.ldq = one_stride(q, pitch, &M);
+        p.ldw = one_stride(w, pitch, &N_rows);
+        if (M > INT32_MAX) throw ValueError("dimensions must fit 32 bits");
+        p.M = (int32_t)M; p.N = (int32_t)N; p.K = (int32_t)K;
+        p.dtype = type == at::kFloat ? TVM_ATTN_FP32 : TVM_ATTN_BF16;
+        std::vector<int64_t> sizes(q.sizes().begin(), q.sizes().end());
+        sizes.back() = N;
+        at::Tensor y = optional_tensor(a[6]);
+        const bool given = y.defined();
+        const c10::cuda::CUDAGuard guard(q.device());
+        if (!given) y = packed(sizes, type, q.device());
+        else if (y.sizes() != at::IntArrayRef(sizes) || y.scalar_type() != type || y.device() != q.device())
+            throw ValueError("`out` must be (..., N) of the result's dtype");
+        p.ldy = one_stride(y, N, &M_out);
+        const c10::cuda::CUDAStream st = stream_of(a[7], q.device());
+        if (!given) used_on(&y, 1, a[7], st);
+        const int rc = without_gil([&] { return p_linear(&p, ptr(q), (float*)ptr(s), ptr(w), (float*)ptr(ws), (float*)ptr(bias), ptr(y), st.stream()); });
+        return rc != TVM_ATTN_OK ? PyLong_FromLong(rc) : THPVariable_Wrap(std::move(y));
+    });
+}
+
+// bind(addresses of tvm_attn_jvp_fwd, _bwd, _bwd_noalloc, _workspace_bytes, tvm_qk_rmsnorm_jvp_fwd, _bwd, _workspace_bytes,
+// tvm_attn_rmsnorm_jvp_fwd, _bwd, _workspace_bytes, tvm_attn_rmsnorm_s8, tvm_attn_quantize_s8, tvm_attn_linear_s8)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 7) { PyErr_SetString(PyExc_TypeError, "seven addresses are needed"); return nullptr; }
-    void* f[7];
-    for (int i = 0; i < 7; ++i) {
+    if (n != 13) { PyErr_SetString(PyExc_TypeError, "thirteen addresses are needed"); return nullptr; }
+    void* f[13];
+    for (int i = 0; i < 13; ++i) {
         f[i] = PyLong_AsVoidPtr(a[i]);
         if (!f[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a null address");
@@ -307,6 +553,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     p_fwd = (decltype(p_fwd))f[0]; p_bwd = (decltype(p_bwd))f[1]; p_bwd_noalloc = (decltype(p_bwd_noalloc))f[2]; p_ws = (decltype(p_ws))f[3];
     p_norm_fwd = (decltype(p_norm_fwd))f[4]; p_norm_bwd = (decltype(p_norm_bwd))f[5]; p_norm_ws = (decltype(p_norm_ws))f[6];
+    p_rows_fwd = (decltype(p_rows_fwd))f[7]; p_rows_bwd = (decltype(p_rows_bwd))f[8]; p_rows_ws = (decltype(p_rows_ws))f[9];
+    p_rows_s8 = (decltype(p_rows_s8))f[10]; p_quantize = (decltype(p_quantize))f[11]; p_linear = (decltype(p_linear))f[12];
     Py_RETURN_NONE;
 }
 
@@ -315,6 +563,10 @@ PyMethodDef methods[] = {{"bind", (PyCFunction)(void*)bind, METH_FASTCALL, nullp
                          {"bwd", (PyCFunction)(void*)bwd, METH_FASTCALL, nullptr},
                          {"norm_fwd", (PyCFunction)(void*)norm_fwd, METH_FASTCALL, nullptr},
                          {"norm_bwd", (PyCFunction)(void*)norm_bwd, METH_FASTCALL, nullptr},
+                         {"rows_fwd", (PyCFunction)(void*)rows_fwd, METH_FASTCALL, nullptr},
+                         {"rows_bwd", (PyCFunction)(void*)rows_bwd, METH_FASTCALL, nullptr},
+                         {"rows_s8", (PyCFunction)(void*)rows_s8, METH_FASTCALL, nullptr},
+                         {"linear_s8", (PyCFunction)(void*)linear_s8, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tvm_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -12,6 +12,7 @@
 #include <mutex>
 #include <utility>
 
+#include "host_common.h"
 #include "jvp_sm100.cuh"
 #include "qk_rmsnorm.cuh"
 #include "rowsums.cuh"
@@ -19,18 +20,9 @@
 
 namespace tvm_attn {
 
-static std::atomic<uint64_t> g_launches{0};
+std::atomic<uint64_t> g_launches{0};
 
 __device__ int g_status_word = 0;  // raised by a tensor-core kernel whose bounded wait ran out
-
-// What a call needs to know about the current device, looked up once per thread and CUDA context (the lookups cost a
-// small call as much as a launch): a context's id is never used again in a process, so a device reset or a switch of
-// devices is a new lookup.
-struct DeviceFacts {
-    unsigned long long ctx = 0;
-    int sms = 0, major = 0;
-    int* status = nullptr;   // device address of g_status_word
-};
 
 // Driver functions, by the runtime's entry-point lookup (the library does not link the driver).
 template <typename F>
@@ -58,7 +50,7 @@ static unsigned long long context_id() {
     return get_id(ctx, &id) == CUDA_SUCCESS ? id : 0;
 }
 
-static const DeviceFacts* device_facts() {
+const DeviceFacts* device_facts() {
     thread_local DeviceFacts facts;
     const unsigned long long ctx = context_id();
     if (ctx == 0) return nullptr;
@@ -74,8 +66,7 @@ static const DeviceFacts* device_facts() {
     return &facts;
 }
 
-// The facts of a device that runs the tensor-core kernels.
-static int tensor_core_device(const DeviceFacts** f) {
+int tensor_core_device(const DeviceFacts** f) {
     *f = device_facts();
     return !*f ? TVM_ATTN_CUDA_ERROR : (*f)->major == 10 ? TVM_ATTN_OK : TVM_ATTN_UNSUPPORTED;
 }
@@ -163,10 +154,6 @@ static int check_params(const tvm_attn_params* p, Shape* s) {
     return TVM_ATTN_OK;
 }
 
-static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-static int cuda_status(cudaError_t e) { return e == cudaSuccess ? TVM_ATTN_OK : TVM_ATTN_CUDA_ERROR; }
-
 // ------------------------------------------------------------------------------------------------
 // CUDA-core path
 template <typename T>
@@ -248,11 +235,7 @@ static int simt_bwd(const Shape& s, const void* Q, const void* K, const void* V,
 
 // ------------------------------------------------------------------------------------------------
 // Tensor-core path
-typedef CUresult (*encode_tiled_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                    const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                    CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static encode_tiled_fn get_encode_fn() {
+encode_tiled_fn get_encode_fn() {
     static const encode_tiled_fn fn = driver_function<encode_tiled_fn>("cuTensorMapEncodeTiled");
     return fn;
 }
