@@ -3,10 +3,17 @@
 // q (M, K) with a scale for each row (token), w (N, K) with a scale for each row (output channel), both K-major; the sum is
 // exact (32-bit integers), the rest is fp32 and rounded once to the output's type.
 //
-// mma.sync with 16 channels and 8 rows a warp: operands go from global memory
+// Many rows: tcgen05.mma kind::i8 (32-bit integer accumulators in tensor memory) on pairs of CTAs, 256 rows x BN channels a
+// tile.  An MMA of a pair reads half of the weights' tile from each CTA's shared memory: tiles of 128 x 256 on single CTAs would
+// load 24 and read 12 KB where these load 16 and read 8, more than the 128 bytes a cycle that shared memory has at the rate of
+// the tensor cores.  Warp 0 loads by TMA, warp 1 of the pair's first CTA issues the MMAs, warps 4 to 11 scale and store one
+// accumulator while the other one fills; a pair walks over its tiles, and the ring of loads runs on through them.
+//
+// Few rows: the weights' bytes are all there is.  mma.sync with 16 channels and 8 rows a warp: operands go from global memory
 // straight to registers (a contraction does not care about the order of k: a lane's 16 contiguous bytes serve as its four
 // operand words), the warps of a block share k, and the partial sums, integers, are added in shared memory.
 #pragma once
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -23,7 +30,10 @@ struct LinearParams {
     void* y;
     long long ldq, ldw, ldy;   // elements between rows
     int M, N, K;
-    int ksplit;          // warps of a block that share k (1, 2, 4, 8)
+    int ksplit;          // few rows: warps of a block that share k (1, 2, 4, 8)
+    int tiles_m, tiles_n;      // many rows
+    int tma_out;               // whether y's rows begin on 16 bytes
+    int* status;               // device status word; non-zero makes the kernel a no-op
 };
 
 template <typename T> __device__ __forceinline__ T linear_round(float v);
@@ -107,6 +117,253 @@ __global__ void __launch_bounds__(LIN_FEW_THREADS) linear_s8_few_kernel(const Li
         const float v = (float)sum * p.s[m] * p.ws[n];
         static_cast<OUT*>(p.y)[m * p.ldy + n] = linear_round<OUT>(p.bias ? v + p.bias[n] : v);
     }
+}
+
+// ------------------------------------------------------------------------------------------------ many rows
+constexpr int LIN_ROWS = 128;          // of a tile, per CTA
+constexpr int LIN_THREADS = 384;
+constexpr int LIN_UNIT = 32;           // columns that an epilogue warp stages and stores at a time
+constexpr int LIN_GROUP = 8;           // tiles of rows that are worked through for all channels before the next ones: 2048 rows stay in L2
+constexpr uint64_t LIN_WAIT_LIMIT_NS = 200ull * 1000ull * 1000ull;
+
+template <int BN, typename OUT>
+struct LinCfg {
+    static constexpr int A_BYTES = LIN_ROWS * 128, B_BYTES = BN / 2 * 128, STAGE = A_BYTES + B_BYTES;
+    static constexpr int BUFS = sizeof(OUT) == 2 ? 2 : 1, BUF_BYTES = 32 * LIN_UNIT * (int)sizeof(OUT);   // of an epilogue warp
+    static constexpr int STAGING = 8 * BUFS * BUF_BYTES, TABLES = 2 * 2 * BN * 4;
+    static constexpr int BARRIERS = 256, MOST = 227 * 1024 - 1024;
+    static constexpr int STAGES = (MOST - STAGING - TABLES - BARRIERS) / STAGE < 8 ? (MOST - STAGING - TABLES - BARRIERS) / STAGE : 8;
+    static constexpr int O_STAGING = STAGES * STAGE, O_TABLES = O_STAGING + STAGING, O_BARRIERS = O_TABLES + TABLES;
+    static constexpr int SMEM_BYTES = O_BARRIERS + BARRIERS + 1024;   // (the base is moved up to 1024 bytes)
+    static constexpr uint32_t ACC_COLS = BN > 128 ? 256 : BN, TMEM_COLS = 2 * ACC_COLS;
+    static_assert(STAGES >= 4 && (2 * STAGES + 5) * 8 + 16 <= BARRIERS && BN % 64 == 0 && BN <= 256, "");
+};
+
+// One of a pair's two CTAs: what its roles share.
+template <int BN, typename OUT>
+struct LinBlock {
+    using C = LinCfg<BN, OUT>;
+    uint32_t base, rank;
+    __device__ __forceinline__ uint32_t bar(int i) const { return base + C::O_BARRIERS + 8 * i; }
+    __device__ __forceinline__ uint32_t full(int s) const { return bar(s); }                        // (the first CTA's) a stage's loads of both CTAs have landed
+    __device__ __forceinline__ uint32_t empty(int s) const { return bar(C::STAGES + s); }           // its MMAs are done
+    __device__ __forceinline__ uint32_t acc_full(int a) const { return bar(2 * C::STAGES + a); }    // a tile's MMAs are done
+    __device__ __forceinline__ uint32_t acc_empty(int a) const { return bar(2 * C::STAGES + 2 + a); }   // (the first CTA's) both CTAs have read it
+    __device__ __forceinline__ uint32_t drain() const { return bar(2 * C::STAGES + 4); }
+    __device__ __forceinline__ uint32_t flags() const { return bar(2 * C::STAGES + 5); }            // abort, skip, tensor-memory address
+    __device__ __forceinline__ bool wait(uint32_t b, uint32_t parity) const { return ptx::mbar_wait_warp_s(b, parity, flags(), LIN_WAIT_LIMIT_NS); }
+};
+
+__device__ __forceinline__ void linear_tile(const LinearParams& p, int tile, int& tm, int& tn) {
+    const int per = LIN_GROUP * p.tiles_n, first = tile / per * LIN_GROUP, rest = tile % per;
+    const int rows = p.tiles_m - first < LIN_GROUP ? p.tiles_m - first : LIN_GROUP;
+    tm = first + rest % rows;
+    tn = rest / rows;
+}
+
+template <int BN, typename OUT>
+__device__ __forceinline__ void linear_load(const LinearParams& p, const LinBlock<BN, OUT>& k, const CUtensorMap& ma, const CUtensorMap& mb, int pair, int pairs) {
+    using C = LinCfg<BN, OUT>;
+    const int tiles = p.tiles_m * p.tiles_n, kblocks = (p.K + 127) / 128;
+    const uint32_t el = ptx::elect_one();
+    int s = 0;
+    uint32_t phase = 1;   // the first pass finds every stage empty
+    for (int tile = pair; tile < tiles; tile += pairs) {
+        int tm, tn;
+        linear_tile(p, tile, tm, tn);
+        const int row_a = tm * 2 * LIN_ROWS + (int)k.rank * LIN_ROWS, row_b = tn * BN + (int)k.rank * (BN / 2);
+        for (int kb = 0; kb < kblocks; ++kb) {
+            if (!k.wait(k.empty(s), phase)) {
+                // loads of this warp may be in flight: they land within microseconds, the block leaves after two milliseconds
+                for (const uint64_t t0 = ptx::globaltimer_ns(); ptx::globaltimer_ns() - t0 < ptx::DRAIN_LIMIT_NS;) __nanosleep(1000);
+                return;
+            }
+            if (el) {
+                const uint32_t full = ptx::cluster_address(k.full(s), 0), to = k.base + s * C::STAGE;
+                if (k.rank == 0) ptx::mbar_arrive_expect_tx(k.full(s), 2 * C::STAGE);
+                ptx::tma_load_2d_pair(to, &ma, full, kb * 128, row_a);
+                ptx::tma_load_2d_pair(to + C::A_BYTES, &mb, full, kb * 128, row_b);
+            }
+            __syncwarp();
+            if (++s == C::STAGES) { s = 0; phase ^= 1; }
+        }
+    }
+    // every arrival that the MMAs still owe this CTA has come in before it leaves
+    for (int i = 0; i < C::STAGES; ++i) {
+        if (!k.wait(k.empty(s), phase)) return;
+        if (++s == C::STAGES) { s = 0; phase ^= 1; }
+    }
+}
+
+template <int BN, typename OUT>
+__device__ __forceinline__ void linear_issue(const LinearParams& p, const LinBlock<BN, OUT>& k, uint32_t tmem, int pair, int pairs) {
+    using C = LinCfg<BN, OUT>;
+    constexpr uint32_t IDESC = ptx::idesc_s8_s32(2 * LIN_ROWS, BN), HI = ptx::desc_hi_sw128(1024);
+    const int tiles = p.tiles_m * p.tiles_n, kblocks = (p.K + 127) / 128;
+    const uint32_t el = ptx::elect_one();
+    int s = 0, n = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int tile = pair; tile < tiles && ok; tile += pairs, ++n) {
+        const int acc = n & 1;
+        ok = k.wait(k.acc_empty(acc), ((n >> 1) & 1) ^ 1);
+        ptx::tc_fence_after_sync();
+        const uint32_t d = tmem + acc * C::ACC_COLS;
+        for (int kb = 0; kb < kblocks && ok; ++kb) {
+            ok = k.wait(k.full(s), phase);
+            if (!ok) break;
+            ptx::tc_fence_after_sync();
+            const uint32_t a = ptx::desc_lo(k.base + s * C::STAGE, 16), b = ptx::desc_lo(k.base + s * C::STAGE + C::A_BYTES, 16);
+            const int steps = p.K - kb * 128 > 96 ? 4 : (p.K - kb * 128 + 31) / 32;   // (behind K there are zeros)
+            for (int i = 0; i < steps; ++i) ptx::mma_s8_pair(el, d, a + 2 * i, b + 2 * i, HI, IDESC, kb + i > 0);
+            ptx::mma_commit_pair(el, k.empty(s));
+            if (++s == C::STAGES) { s = 0; phase ^= 1; }
+        }
+        if (ok) ptx::mma_commit_pair(el, k.acc_full(acc));
+    }
+    if (!ok) {   // the MMAs in flight end before the tensor memory is freed
+        ptx::mma_commit_pair(el, k.drain());
+        ptx::mbar_wait_drain(k.drain(), 0, ptx::DRAIN_LIMIT_NS);
+    }
+}
+
+template <int BN, typename OUT>
+__device__ __forceinline__ void linear_store(const LinearParams& p, const LinBlock<BN, OUT>& k, const CUtensorMap& my, uint32_t tmem, int pair, int pairs) {
+    using C = LinCfg<BN, OUT>;
+    constexpr int PER16 = 16 / (int)sizeof(OUT), PIECES = LIN_UNIT / PER16;   // 16-byte pieces of a staged row: 4 (bf16) or 8
+    const int tiles = p.tiles_m * p.tiles_n, lane = threadIdx.x & 31, warp = threadIdx.x / 32 - 4, quad = warp & 3, half = warp >> 2;
+    const int thread = threadIdx.x - 128;
+    const uint32_t staging = k.base + C::O_STAGING + warp * C::BUFS * C::BUF_BYTES, tables = k.base + C::O_TABLES;
+    const uint32_t acc_empty = ptx::cluster_address(k.acc_empty(0), 0);
+    uint32_t buf = 0;
+    int n = 0;
+    bool ok = true;
+    for (int tile = pair; tile < tiles; tile += pairs, ++n) {
+        int tm, tn;
+        linear_tile(p, tile, tm, tn);
+        const int acc = n & 1, col0 = tn * BN;
+        const long long row0 = (long long)tm * 2 * LIN_ROWS + k.rank * LIN_ROWS + quad * 32, m = row0 + lane;
+        // the channels' scales and biases, in two tables that tiles take in turn: no warp is two tiles ahead of another one
+        const uint32_t table = tables + acc * 2 * BN * 4;
+        if (thread < BN) {
+            const bool in = col0 + thread < p.N;
+            const float a = in ? __ldg(p.ws + col0 + thread) : 0.f, b = in && p.bias ? __ldg(p.bias + col0 + thread) : 0.f;
+            asm volatile("st.shared.f32 [%0], %1;" ::"r"(table + 4 * thread), "f"(a) : "memory");
+            asm volatile("st.shared.f32 [%0], %1;" ::"r"(table + 4 * (BN + thread)), "f"(b) : "memory");
+        }
+        const float sm = m < p.M ? __ldg(p.s + m) : 0.f;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        ok = ok && k.wait(k.acc_full(acc), (n >> 1) & 1);
+        if (!ok) continue;   // (gave up; but the other warps count on this one at the barrier above)
+        ptx::tc_fence_after_sync();
+        const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc * C::ACC_COLS + half * (BN / 2);
+#pragma unroll 1
+        for (int u = 0; u < BN / 2 / LIN_UNIT; ++u) {
+            const int c = half * (BN / 2) + u * LIN_UNIT;
+            uint32_t r[LIN_UNIT];
+            ptx::tmem_ld32(from + u * LIN_UNIT, r);
+            ptx::tmem_wait_ld();
+            if (u == BN / 2 / LIN_UNIT - 1) {   // the accumulator may be filled again
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive_cluster(acc_empty + 8 * acc);
+            }
+            const uint32_t to = staging + buf * C::BUF_BYTES;
+            if (lane == 0) ptx::bulk_wait_read<C::BUFS - 1>();   // the store that read this buffer last is done with it
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j) {
+                uint32_t w[4];
+                float v[PER16];
+#pragma unroll
+                for (int e = 0; e < PER16; e += 4) {
+                    float4 a, b;
+                    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(a.x), "=f"(a.y), "=f"(a.z), "=f"(a.w) : "r"(table + 4 * (c + j * PER16 + e)));
+                    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(table + 4 * (BN + c + j * PER16 + e)));
+                    const uint32_t* q = r + j * PER16 + e;
+                    v[e] = fmaf((float)(int)q[0] * sm, a.x, b.x);
+                    v[e + 1] = fmaf((float)(int)q[1] * sm, a.y, b.y);
+                    v[e + 2] = fmaf((float)(int)q[2] * sm, a.z, b.z);
+                    v[e + 3] = fmaf((float)(int)q[3] * sm, a.w, b.w);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (sizeof(OUT) == 2) w[e] = ptx::pack_bf16(v[2 * e], v[2 * e + 1]);
+                    else w[e] = __float_as_uint(v[e]);
+                }
+                // rows of 64 or 128 bytes, with the swizzle of the tensor map: conflict-free, and what the store expects
+                const int piece = sizeof(OUT) == 2 ? j ^ ((lane >> 1) & 3) : j ^ (lane & 7);
+                ptx::st_shared_v4(to + lane * (LIN_UNIT * (int)sizeof(OUT)) + piece * 16, w[0], w[1], w[2], w[3]);
+            }
+            if (p.tma_out) {
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    if (row0 < p.M && col0 + c < p.N) ptx::tma_store_2d(&my, to, col0 + c, (int)row0);
+                    ptx::bulk_commit();
+                }
+            } else {   // rows that do not begin on 16 bytes: a warp stores one row after the other
+                __syncwarp();
+                const int col = col0 + c + lane;
+                for (int i = 0; i < 32 && row0 + i < p.M; ++i) {
+                    const int piece = sizeof(OUT) == 2 ? (lane / PER16) ^ ((i >> 1) & 3) : (lane / PER16) ^ (i & 7);
+                    const uint32_t at = to + i * (LIN_UNIT * (int)sizeof(OUT)) + piece * 16 + lane % PER16 * (int)sizeof(OUT);
+                    OUT* dst = static_cast<OUT*>(p.y) + (row0 + i) * p.ldy + col;
+                    if constexpr (sizeof(OUT) == 2) {
+                        unsigned short v;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+                        if (col < p.N) *reinterpret_cast<unsigned short*>(dst) = v;
+                    } else {
+                        float v;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
+                        if (col < p.N) *dst = v;
+                    }
+                }
+                __syncwarp();
+            }
+            buf = buf + 1 == C::BUFS ? 0 : buf + 1;
+        }
+    }
+    if (lane == 0) ptx::bulk_wait_all();
+}
+
+template <int BN, typename OUT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LIN_THREADS, 1)
+linear_s8_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, const __grid_constant__ CUtensorMap my, const LinearParams p) {
+    using C = LinCfg<BN, OUT>;
+    extern __shared__ uint8_t smem[];
+    LinBlock<BN, OUT> k;
+    k.base = (ptx::smem_u32(smem) + 1023u) & ~1023u;
+    k.rank = ptx::cluster_rank();
+    const int warp = threadIdx.x >> 5, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    volatile int* flags = static_cast<volatile int*>(__cvta_shared_to_generic(k.flags()));
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) { ptx::mbar_init(k.full(s), 1); ptx::mbar_init(k.empty(s), 1); }
+        for (int a = 0; a < 2; ++a) { ptx::mbar_init(k.acc_full(a), 1); ptx::mbar_init(k.acc_empty(a), 2 * 8); }
+        ptx::mbar_init(k.drain(), 1);
+        flags[0] = 0;
+        flags[1] = *reinterpret_cast<volatile int*>(p.status);   // an earlier kernel timed out: both CTAs do nothing if either sees it
+        ptx::fence_mbar_init();
+    }
+    __syncwarp();
+    ptx::cluster_sync();
+    const bool skip = ptx::ld_cluster(ptx::cluster_address(k.flags() + 4, 0)) | ptx::ld_cluster(ptx::cluster_address(k.flags() + 4, 1));
+    if (warp == 2) ptx::tmem_alloc_pair(k.flags() + 8, C::TMEM_COLS);
+    ptx::tc_fence_before_sync();
+    ptx::cluster_sync();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = flags[2];
+    if (!skip) {
+        if (warp == 0) linear_load<BN, OUT>(p, k, ma, mb, pair, pairs);
+        else if (warp == 1 && k.rank == 0) linear_issue<BN, OUT>(p, k, tmem, pair, pairs);
+        else if (warp >= 4) linear_store<BN, OUT>(p, k, my, tmem, pair, pairs);
+    }
+    __syncwarp();
+    ptx::tc_fence_before_sync();
+    ptx::cluster_sync();   // neither CTA leaves, or frees its tensor memory, while the other one may still reach into it
+    ptx::tc_fence_after_sync();
+    if (warp == 2) ptx::tmem_dealloc_pair(tmem, C::TMEM_COLS);
+    if (threadIdx.x == 0 && flags[0]) atomicExch(p.status, 1);
 }
 
 }  // namespace tvm_attn

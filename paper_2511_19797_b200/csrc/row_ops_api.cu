@@ -266,6 +266,73 @@ static int linear_few(LinearParams p, cudaStream_t st) {
     return launch_few<OUT, 8>(p, st);
 }
 
+// A matrix (rows, cols) in boxes of box_cols x box_rows; what lies outside it reads as zero and is not written.
+static int matrix_map(CUtensorMap* m, CUtensorMapDataType type, int size, const void* ptr, long long cols, long long rows, long long pitch, int box_cols, int box_rows,
+                      CUtensorMapSwizzle swizzle) {
+    encode_tiled_fn fn = get_encode_fn();
+    if (!fn) return TVM_ATTN_CUDA_ERROR;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)(pitch * size)};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, step[2] = {1, 1};
+    return fn(m, type, 2, const_cast<void*>(ptr), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? TVM_ATTN_OK : TVM_ATTN_CUDA_ERROR;
+}
+
+template <int BN, typename OUT>
+static int launch_many(LinearParams p, const DeviceFacts& dev, cudaStream_t st) {
+    using C = LinCfg<BN, OUT>;
+    constexpr auto kern = linear_s8_kernel<BN, OUT>;
+    thread_local unsigned long long prepared = 0;   // once per thread and context
+    if (prepared != dev.ctx) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES) != cudaSuccess) { cudaGetLastError(); return TVM_ATTN_CUDA_ERROR; }
+        prepared = dev.ctx;
+    }
+    constexpr bool HALF = sizeof(OUT) == 2;
+    CUtensorMap ma, mb, my;
+    int rc = matrix_map(&ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.q, p.K, p.M, p.ldq, 128, LIN_ROWS, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc == TVM_ATTN_OK) rc = matrix_map(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.w, p.K, p.N, p.ldw, 128, BN / 2, CU_TENSOR_MAP_SWIZZLE_128B);
+    my = ma;   // (not used where y's rows do not begin on 16 bytes)
+    p.tma_out = aligned16(p.y) && p.ldy * (long long)sizeof(OUT) % 16 == 0;
+    if (rc == TVM_ATTN_OK && p.tma_out)
+        rc = matrix_map(&my, HALF ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, (int)sizeof(OUT), p.y, p.N, p.M, p.ldy, LIN_UNIT, 32,
+                        HALF ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc != TVM_ATTN_OK) return rc;
+    p.tiles_m = (p.M + 2 * LIN_ROWS - 1) / (2 * LIN_ROWS);
+    p.tiles_n = (p.N + BN - 1) / BN;
+    p.status = dev.status;
+    const long long tiles = (long long)p.tiles_m * p.tiles_n;
+    kern<<<2 * fewer(tiles, dev.sms / 2), LIN_THREADS, C::SMEM_BYTES, st>>>(ma, mb, my, p);
+    g_launches += 1;
+    return cuda_status(cudaGetLastError());
+}
+
+template <typename OUT>
+static int linear_many(const LinearParams& p, cudaStream_t st) {
+    const DeviceFacts* dev;
+    const int rc = tensor_core_device(&dev);
+    if (rc != TVM_ATTN_OK) return rc;
+    // the width of a tile: the one whose rounds of tiles take least, a tile of BN channels counted as BN + 32
+    const long long tiles_m = (p.M + 2 * LIN_ROWS - 1) / (2 * LIN_ROWS), pairs = dev->sms / 2;
+    if (tiles_m * ((p.N + 63) / 64) > 2147483647LL) return TVM_ATTN_UNSUPPORTED;
+    int best = 256;
+    long long least = -1;
+    for (int bn : {256, 192, 128, 64}) {
+        const long long rounds = (tiles_m * ((p.N + bn - 1) / bn) + pairs - 1) / pairs, cost = rounds * (bn + 32);
+        if (least < 0 || cost < least) { least = cost; best = bn; }
+    }
+    switch (best) {
+        case 256: return launch_many<256, OUT>(p, *dev, st);
+        case 192: return launch_many<192, OUT>(p, *dev, st);
+        case 128: return launch_many<128, OUT>(p, *dev, st);
+        default: return launch_many<64, OUT>(p, *dev, st);
+    }
+}
+
+// Up to this many rows the weights' bytes are what a product costs.
+constexpr int LIN_FEW_ROWS = 64;
+
+template <typename OUT>
+static int linear(const LinearParams& p, cudaStream_t st) { return p.M <= LIN_FEW_ROWS ? linear_few<OUT>(p, st) : linear_many<OUT>(p, st); }
+
 }  // namespace tvm_attn
 
 extern "C" int tvm_attn_linear_s8(const tvm_attn_linear_params* p, const void* q, const float* s, const void* w, const float* ws, const float* bias,
@@ -287,5 +354,5 @@ extern "C" int tvm_attn_linear_s8(const tvm_attn_linear_params* p, const void* q
     k.ldq = ldq; k.ldw = ldw; k.ldy = ldy;
     k.M = p->M; k.N = p->N; k.K = p->K;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return p->dtype == TVM_ATTN_FP32 ? linear_few<float>(k, st) : linear_few<__nv_bfloat16>(k, st);
+    return p->dtype == TVM_ATTN_FP32 ? linear<float>(k, st) : linear<__nv_bfloat16>(k, st);
 }
