@@ -122,15 +122,15 @@ __global__ void __launch_bounds__(LIN_FEW_THREADS) linear_s8_few_kernel(const Li
 // ------------------------------------------------------------------------------------------------ many rows
 constexpr int LIN_ROWS = 128;          // of a tile, per CTA
 constexpr int LIN_THREADS = 384;
-constexpr int LIN_UNIT = 32;           // columns that an epilogue warp stages and stores at a time
 constexpr int LIN_GROUP = 8;           // tiles of rows that are worked through for all channels before the next ones: 2048 rows stay in L2
 constexpr uint64_t LIN_WAIT_LIMIT_NS = 200ull * 1000ull * 1000ull;
 
 template <int BN, typename OUT>
 struct LinCfg {
     static constexpr int A_BYTES = LIN_ROWS * 128, B_BYTES = BN / 2 * 128, STAGE = A_BYTES + B_BYTES;
-    static constexpr int BUFS = sizeof(OUT) == 2 ? 2 : 1, BUF_BYTES = 32 * LIN_UNIT * (int)sizeof(OUT);   // of an epilogue warp
-    static constexpr int STAGING = 8 * BUFS * BUF_BYTES, TABLES = 2 * 2 * BN * 4;
+    // The epilogue works on units of 128 bytes of 32 rows, which its eight warps, two for each 32 rows of the accumulator, take in turn.
+    static constexpr int UNIT = 128 / (int)sizeof(OUT), UNITS = BN / UNIT, WARP_UNITS = (UNITS + 1) / 2, UNIT_BYTES = 32 * 128;
+    static constexpr int BUFS = 2, STAGING = 8 * BUFS * UNIT_BYTES, WARP_COLS = WARP_UNITS * UNIT, TABLES = 8 * 2 * WARP_COLS * 4;
     static constexpr int BARRIERS = 256, MOST = 227 * 1024 - 1024;
     static constexpr int STAGES = (MOST - STAGING - TABLES - BARRIERS) / STAGE < 8 ? (MOST - STAGING - TABLES - BARRIERS) / STAGE : 8;
     static constexpr int O_STAGING = STAGES * STAGE, O_TABLES = O_STAGING + STAGING, O_BARRIERS = O_TABLES + TABLES;
@@ -230,98 +230,120 @@ __device__ __forceinline__ void linear_issue(const LinearParams& p, const LinBlo
 template <int BN, typename OUT>
 __device__ __forceinline__ void linear_store(const LinearParams& p, const LinBlock<BN, OUT>& k, const CUtensorMap& my, uint32_t tmem, int pair, int pairs) {
     using C = LinCfg<BN, OUT>;
-    constexpr int PER16 = 16 / (int)sizeof(OUT), PIECES = LIN_UNIT / PER16;   // 16-byte pieces of a staged row: 4 (bf16) or 8
-    const int tiles = p.tiles_m * p.tiles_n, lane = threadIdx.x & 31, warp = threadIdx.x / 32 - 4, quad = warp & 3, half = warp >> 2;
-    const int thread = threadIdx.x - 128;
-    const uint32_t staging = k.base + C::O_STAGING + warp * C::BUFS * C::BUF_BYTES, tables = k.base + C::O_TABLES;
+    constexpr int PER16 = 16 / (int)sizeof(OUT), COLS = (C::WARP_COLS + 31) / 32;
+    const int tiles = p.tiles_m * p.tiles_n, lane = threadIdx.x & 31, warp = threadIdx.x / 32 - 4, quad = warp & 3, side = warp >> 2;
+    const uint32_t staging = k.base + C::O_STAGING + warp * C::BUFS * C::UNIT_BYTES, table = k.base + C::O_TABLES + warp * 2 * C::WARP_COLS * 4;
     const uint32_t acc_empty = ptx::cluster_address(k.acc_empty(0), 0);
+    // A tile's scales: the lane's row's, and those and the biases of the columns of the warp's units (unit 2 j + its turn), a lane's
+    // share of them.  They are loaded a tile ahead and handed out through a table of the warp's own.
+    float sm, wsc[COLS], bia[COLS];
+    auto fetch = [&](int tile, int n) {
+        if (tile >= tiles) return;
+        int tm, tn;
+        linear_tile(p, tile, tm, tn);
+        const long long m = (long long)tm * 2 * LIN_ROWS + k.rank * LIN_ROWS + quad * 32 + lane;
+        sm = m < p.M ? __ldg(p.s + m) : 0.f;
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) {
+            const int at = 32 * j + lane, unit = 2 * (at / C::UNIT) + ((side + n) & 1), col = tn * BN + unit * C::UNIT + at % C::UNIT;
+            const bool in = unit < C::UNITS && col < p.N;
+            wsc[j] = in ? __ldg(p.ws + col) : 0.f;
+            bia[j] = in && p.bias ? __ldg(p.bias + col) : 0.f;
+        }
+    };
+    fetch(pair, 0);
     uint32_t buf = 0;
     int n = 0;
-    bool ok = true;
     for (int tile = pair; tile < tiles; tile += pairs, ++n) {
         int tm, tn;
         linear_tile(p, tile, tm, tn);
-        const int acc = n & 1, col0 = tn * BN;
-        const long long row0 = (long long)tm * 2 * LIN_ROWS + k.rank * LIN_ROWS + quad * 32, m = row0 + lane;
-        // the channels' scales and biases, in two tables that tiles take in turn: no warp is two tiles ahead of another one
-        const uint32_t table = tables + acc * 2 * BN * 4;
-        if (thread < BN) {
-            const bool in = col0 + thread < p.N;
-            const float a = in ? __ldg(p.ws + col0 + thread) : 0.f, b = in && p.bias ? __ldg(p.bias + col0 + thread) : 0.f;
-            asm volatile("st.shared.f32 [%0], %1;" ::"r"(table + 4 * thread), "f"(a) : "memory");
-            asm volatile("st.shared.f32 [%0], %1;" ::"r"(table + 4 * (BN + thread)), "f"(b) : "memory");
+        const int acc = n & 1, turn = (side + n) & 1;
+        const long long row0 = (long long)tm * 2 * LIN_ROWS + k.rank * LIN_ROWS + quad * 32;
+        const float s_row = sm;
+        __syncwarp();   // the tile before is done with the table
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) {
+            asm volatile("st.shared.f32 [%0], %1;" ::"r"(table + 4 * (32 * j + lane)), "f"(wsc[j]) : "memory");
+            asm volatile("st.shared.f32 [%0], %1;" ::"r"(table + 4 * (C::WARP_COLS + 32 * j + lane)), "f"(bia[j]) : "memory");
         }
-        const float sm = m < p.M ? __ldg(p.s + m) : 0.f;
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        ok = ok && k.wait(k.acc_full(acc), (n >> 1) & 1);
-        if (!ok) continue;   // (gave up; but the other warps count on this one at the barrier above)
+        __syncwarp();
+        fetch(tile + pairs, n + 1);
+        if (!k.wait(k.acc_full(acc), (n >> 1) & 1)) break;
         ptx::tc_fence_after_sync();
-        const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc * C::ACC_COLS + half * (BN / 2);
+        const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc * C::ACC_COLS;
+        const uint64_t s2 = ptx::pack2(s_row, s_row);
 #pragma unroll 1
-        for (int u = 0; u < BN / 2 / LIN_UNIT; ++u) {
-            const int c = half * (BN / 2) + u * LIN_UNIT;
-            uint32_t r[LIN_UNIT];
-            ptx::tmem_ld32(from + u * LIN_UNIT, r);
-            ptx::tmem_wait_ld();
-            if (u == BN / 2 / LIN_UNIT - 1) {   // the accumulator may be filled again
+        for (int j = 0, u = turn; j < C::WARP_UNITS; ++j, u += 2) {
+            const bool there = u < C::UNITS, last = u + 2 >= C::UNITS;
+            uint32_t r[C::UNIT];
+            if (there) {
+#pragma unroll
+                for (int c = 0; c < C::UNIT; c += 32) ptx::tmem_ld32(from + u * C::UNIT + c, r + c);
+                ptx::tmem_wait_ld();
+            }
+            if (last) {   // the accumulator may be filled again
                 ptx::tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive_cluster(acc_empty + 8 * acc);
             }
-            const uint32_t to = staging + buf * C::BUF_BYTES;
+            if (!there) break;
+            const uint32_t to = staging + buf * C::UNIT_BYTES;
             if (lane == 0) ptx::bulk_wait_read<C::BUFS - 1>();   // the store that read this buffer last is done with it
             __syncwarp();
 #pragma unroll
-            for (int j = 0; j < PIECES; ++j) {
-                uint32_t w[4];
-                float v[PER16];
+            for (int i = 0; i < 8; ++i) {   // pieces of 16 bytes
+                uint64_t v[PER16 / 2];
 #pragma unroll
                 for (int e = 0; e < PER16; e += 4) {
-                    float4 a, b;
-                    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(a.x), "=f"(a.y), "=f"(a.z), "=f"(a.w) : "r"(table + 4 * (c + j * PER16 + e)));
-                    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(table + 4 * (BN + c + j * PER16 + e)));
-                    const uint32_t* q = r + j * PER16 + e;
-                    v[e] = fmaf((float)(int)q[0] * sm, a.x, b.x);
-                    v[e + 1] = fmaf((float)(int)q[1] * sm, a.y, b.y);
-                    v[e + 2] = fmaf((float)(int)q[2] * sm, a.z, b.z);
-                    v[e + 3] = fmaf((float)(int)q[3] * sm, a.w, b.w);
+                    const uint32_t at = table + 4 * (j * C::UNIT + i * PER16 + e);
+                    uint64_t a[2], b[2];
+                    asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(a[0]), "=l"(a[1]) : "r"(at));
+                    asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(b[0]), "=l"(b[1]) : "r"(at + 4 * C::WARP_COLS));
+                    const uint32_t* q = r + i * PER16 + e;
+                    v[e / 2] = ptx::fma2(ptx::mul2(ptx::pack2((float)(int)q[0], (float)(int)q[1]), s2), a[0], b[0]);
+                    v[e / 2 + 1] = ptx::fma2(ptx::mul2(ptx::pack2((float)(int)q[2], (float)(int)q[3]), s2), a[1], b[1]);
                 }
+                uint32_t w[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (sizeof(OUT) == 2) w[e] = ptx::pack_bf16(v[2 * e], v[2 * e + 1]);
-                    else w[e] = __float_as_uint(v[e]);
+                for (int e = 0; e < PER16 / 2; ++e) {
+                    float lo, hi;
+                    ptx::unpack2(v[e], lo, hi);
+                    if constexpr (sizeof(OUT) == 2) w[e] = ptx::pack_bf16(lo, hi);
+                    else { w[2 * e] = __float_as_uint(lo); w[2 * e + 1] = __float_as_uint(hi); }
                 }
-                // rows of 64 or 128 bytes, with the swizzle of the tensor map: conflict-free, and what the store expects
-                const int piece = sizeof(OUT) == 2 ? j ^ ((lane >> 1) & 3) : j ^ (lane & 7);
-                ptx::st_shared_v4(to + lane * (LIN_UNIT * (int)sizeof(OUT)) + piece * 16, w[0], w[1], w[2], w[3]);
+                // rows of 128 bytes with the swizzle of the tensor map: free of bank conflicts, and what the store expects
+                ptx::st_shared_v4(to + lane * 128 + ((i ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
             }
+            const int col0 = tn * BN + u * C::UNIT;
             if (p.tma_out) {
                 ptx::fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    if (row0 < p.M && col0 + c < p.N) ptx::tma_store_2d(&my, to, col0 + c, (int)row0);
+                    if (row0 < p.M && col0 < p.N) ptx::tma_store_2d(&my, to, col0, (int)row0);
                     ptx::bulk_commit();
                 }
             } else {   // rows that do not begin on 16 bytes: a warp stores one row after the other
                 __syncwarp();
-                const int col = col0 + c + lane;
                 for (int i = 0; i < 32 && row0 + i < p.M; ++i) {
-                    const int piece = sizeof(OUT) == 2 ? (lane / PER16) ^ ((i >> 1) & 3) : (lane / PER16) ^ (i & 7);
-                    const uint32_t at = to + i * (LIN_UNIT * (int)sizeof(OUT)) + piece * 16 + lane % PER16 * (int)sizeof(OUT);
-                    OUT* dst = static_cast<OUT*>(p.y) + (row0 + i) * p.ldy + col;
-                    if constexpr (sizeof(OUT) == 2) {
-                        unsigned short v;
-                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
-                        if (col < p.N) *reinterpret_cast<unsigned short*>(dst) = v;
-                    } else {
-                        float v;
-                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
-                        if (col < p.N) *dst = v;
+                    OUT* dst = static_cast<OUT*>(p.y) + (row0 + i) * p.ldy + col0;
+#pragma unroll
+                    for (int c = lane; c < C::UNIT; c += 32) {
+                        const uint32_t at = to + i * 128 + (((c / PER16) ^ (i & 7)) << 4) + c % PER16 * (int)sizeof(OUT);
+                        if constexpr (sizeof(OUT) == 2) {
+                            unsigned short v;
+                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+                            if (col0 + c < p.N) *reinterpret_cast<unsigned short*>(dst + c) = v;
+                        } else {
+                            float v;
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
+                            if (col0 + c < p.N) dst[c] = v;
+                        }
                     }
                 }
                 __syncwarp();
             }
-            buf = buf + 1 == C::BUFS ? 0 : buf + 1;
+            buf ^= 1;
+            if (last) break;
         }
     }
     if (lane == 0) ptx::bulk_wait_all();

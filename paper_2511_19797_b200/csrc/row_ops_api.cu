@@ -293,8 +293,8 @@ static int launch_many(LinearParams p, const DeviceFacts& dev, cudaStream_t st) 
     my = ma;   // (not used where y's rows do not begin on 16 bytes)
     p.tma_out = aligned16(p.y) && p.ldy * (long long)sizeof(OUT) % 16 == 0;
     if (rc == TVM_ATTN_OK && p.tma_out)
-        rc = matrix_map(&my, HALF ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, (int)sizeof(OUT), p.y, p.N, p.M, p.ldy, LIN_UNIT, 32,
-                        HALF ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B);
+        rc = matrix_map(&my, HALF ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, (int)sizeof(OUT), p.y, p.N, p.M, p.ldy, C::UNIT, 32,
+                        CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc != TVM_ATTN_OK) return rc;
     p.tiles_m = (p.M + 2 * LIN_ROWS - 1) / (2 * LIN_ROWS);
     p.tiles_n = (p.N + BN - 1) / BN;
