@@ -310,13 +310,14 @@ static int linear_many(const LinearParams& p, cudaStream_t st) {
     const DeviceFacts* dev;
     const int rc = tensor_core_device(&dev);
     if (rc != TVM_ATTN_OK) return rc;
-    // the width of a tile: the one whose rounds of tiles take least, a tile of BN channels counted as BN + 32
+    // the width of a tile: the one whose rounds of tiles take least.  What an SM loads bounds them (62 bytes a cycle from L2,
+    // 128 + BN / 2 rows of k for each of a pair's CTAs: 446 cycles per 128 bytes of k at 192 channels, 402 at 128), not its MMAs
     const long long tiles_m = (p.M + 2 * LIN_ROWS - 1) / (2 * LIN_ROWS), pairs = dev->sms / 2;
     if (tiles_m * ((p.N + 63) / 64) > 2147483647LL) return TVM_ATTN_UNSUPPORTED;
     int best = 256;
     long long least = -1;
     for (int bn : {256, 192, 128, 64}) {
-        const long long rounds = (tiles_m * ((p.N + bn - 1) / bn) + pairs - 1) / pairs, cost = rounds * (bn + 32);
+        const long long rounds = (tiles_m * ((p.N + bn - 1) / bn) + pairs - 1) / pairs, cost = rounds * (256 + bn);
         if (least < 0 || cost < least) { least = cost; best = bn; }
     }
     switch (best) {
