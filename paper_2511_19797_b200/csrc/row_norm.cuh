@@ -3,10 +3,11 @@
 // replaced by RMSNorm without a learnable scale; App. "Lipschitzness of RMSNorm" for the Jacobian).  Per row of D elements:
 //     h = x + res     r = sqrt(mean(h^2) + eps)     u = h / r     y = g u
 //     th = tx + tres                                ty = g J th   with J v = (v - u (u . v) / D) / r
-// Streaming work, every tensor read or written once.  A row stays in registers between its loads and its stores, as fp32: up to
-// 5 chunks of 16 bytes on each of P <= 32 lanes of a warp, or 3 or 4 on each thread of a block of its own.  The sums over a
-// row, the dot products and the scale's gradient are fp32.  The norm is that of the sum before it is rounded to the type
-// that h is stored in.
+// Streaming work, every tensor read or written once, bound by HBM once enough bytes are in flight.  A row has a 16-byte chunk on
+// each of P lanes of a warp, or 1, 2 or 4 chunks on each thread of a block of its own, and stays in registers between its loads
+// and its stores: few registers a thread, so that the blocks of an SM, each a row further on, cover for one another.  The sums over a
+// row, the dot products and the scale's gradient are fp32.  The norm is that of the sum before it is rounded to the type that h is
+// stored in.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -33,16 +34,17 @@ struct RowNormParams {
     bool norm;        // 8-bit rows: of the norm's output (else of x + res itself)
 };
 
-// A warp's rows: at most this many chunks a lane; wider rows get a block.
-constexpr int ROWNORM_WARP_CHUNKS = 5;
-constexpr int ROWNORM_THREADS = 256;       // forward, rows on warps
-constexpr int ROWNORM_BWD_THREADS = 128;   // backward, rows on warps
-
-// Threads that a block with one row can have: 16384 elements at 4 chunks a thread.
-template <typename T> constexpr int rownorm_block_threads() { return 16384 * (int)sizeof(T) / 64; }
-// Blocks of the backward at most.  A fixed number: the partial sums of the scale's gradient, a row per block, have a size
-// and an order that do not depend on the device.  `warps`: of a block with one row, 0 for rows on warps.
-__host__ __device__ constexpr int rownorm_bwd_blocks(int warps) { return 148 * (warps == 0 ? 3 : warps < 12 ? 12 / warps : 1); }
+constexpr int ROWNORM_THREADS = 256;   // of a block whose rows are on warps
+// Threads that a block with one row can have, C chunks each.
+template <typename T, int C> constexpr int rownorm_block_threads() { return C == 4 && sizeof(T) == 4 ? 1024 : C == 1 ? 160 : 512; }
+// Blocks of the backward on an SM: as many as the registers let in (a block walks over its rows from the start to the end of the
+// launch, so one that waits for another's end would double the time).  `threads`: of a block with one row, 0 for rows on warps.
+__host__ __device__ constexpr int rownorm_bwd_resident(int threads, bool tan) {
+    return threads == 0 ? (tan ? 2 : 4) : threads <= 160 ? (tan ? 4 : 7) : threads <= 256 ? 2 : 1;
+}
+// All of them.  A fixed number: the partial sums of the scale's gradient, a row per block, have a size and an order that do not
+// depend on the device.
+__host__ __device__ constexpr int rownorm_bwd_blocks(int threads, bool tan) { return 148 * rownorm_bwd_resident(threads, tan); }
 
 // The lanes of one row and their columns.  VEC: a chunk is 16 contiguous bytes.  Otherwise (a pointer, stride or width that is
 // no multiple of 16 bytes) the elements of a chunk are P apart, so that an instruction still touches contiguous bytes.
@@ -114,32 +116,66 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // a NaN on eithe
     return r;
 }
 
-// N sums over a row (the last one a maximum with MAX), returned to all its lanes, the same bits on each.  `slot`: shared
-// memory of a block with one row, 32 N floats; two of them are used in turn, so that one barrier a reduction is enough.
+// N sums over a row (the last one a maximum with MAX), returned to all its lanes, the same bits on each.  In a block with one row
+// the lanes of a warp halve the values among them with every step (8 shuffles for 5 values, not 25), a lane writes each to `slot`, 32 N
+// floats of shared memory that are zero behind the block's warps, and all threads add the warps' parts up in the same order.  Two
+// slots are used in turn, so that one barrier a reduction is enough.
 template <int N, bool MAX, bool BLOCK>
 __device__ __forceinline__ void row_reduce(float (&v)[N], int P, float* slot) {
-    const int lanes = BLOCK ? 32 : P;
-    for (int off = lanes >> 1; off > 0; off >>= 1)
+    if constexpr (!BLOCK) {
+        for (int off = P >> 1; off > 0; off >>= 1)
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const float w = __shfl_xor_sync(0xffffffffu, v[k], off);
-            v[k] = MAX && k == N - 1 ? max_nan(v[k], w) : v[k] + w;
-        }
-    if constexpr (BLOCK) {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-        if (lane == 0)
-#pragma unroll
-            for (int k = 0; k < N; ++k) slot[32 * k + warp] = v[k];
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            v[k] = lane < warps ? slot[32 * k + lane] : 0.f;   // (the maximum is one of magnitudes)
-            for (int off = 16; off > 0; off >>= 1) {
+            for (int k = 0; k < N; ++k) {
                 const float w = __shfl_xor_sync(0xffffffffu, v[k], off);
                 v[k] = MAX && k == N - 1 ? max_nan(v[k], w) : v[k] + w;
             }
+    } else {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+        float part[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) part[k] = v[k];
+        int id = 0, left = N;   // the first of the `left` values that this lane still holds (padding among them)
+        bool real = true;
+        int n = N;
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) {
+            const bool high = lane & off;
+            if (n > 1) {
+                const int half = (n + 1) / 2;
+#pragma unroll
+                for (int k = 0; k < (N + 1) / 2; ++k) {
+                    if (k >= half) continue;
+                    const float lo = part[k], hi = k + half < n ? part[k + half < N ? k + half : 0] : 0.f;
+                    const float keep = high ? hi : lo, w = __shfl_xor_sync(0xffffffffu, high ? lo : hi, off);
+                    part[k] = MAX && high ? max_nan(keep, w) : keep + w;   // (MAX: N = 2, the high lanes have the maximum)
+                }
+                id += high ? half : 0;
+                left = high ? left - half : left < half ? left : half;
+                real = real && left > 0;
+                n = half;
+            } else {
+                const float w = __shfl_xor_sync(0xffffffffu, part[0], off);
+                part[0] = MAX && id == N - 1 ? max_nan(part[0], w) : part[0] + w;
+            }
+        }
+        constexpr int SAME = N == 1 ? 31 : N == 2 ? 15 : 3;   // lanes that differ in these bits hold the same value
+        if ((lane & SAME) == 0 && real) slot[32 * id + warp] = part[0];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            float sum = 0.f;
+            for (int w = 0; w < warps; w += 4) {
+                const float4 q = *reinterpret_cast<const float4*>(slot + 32 * k + w);
+                sum = MAX && k == N - 1 ? max_nan(sum, max_nan(max_nan(q.x, q.y), max_nan(q.z, q.w))) : sum + ((q.x + q.y) + (q.z + q.w));
+            }
+            v[k] = sum;   // (the maximum is one of magnitudes)
         }
     }
+}
+// Zeros in the slots, for all threads of the block.
+__device__ __forceinline__ void clear_slots(float* slots, int n) {
+    for (int i = threadIdx.x; i < n; i += blockDim.x) slots[i] = 0.f;
+    __syncthreads();
 }
 
 // The power of two that a row's elements are multiplied by in its sum of squares, when that sum left the range of fp32 at `pre` =
@@ -153,12 +189,13 @@ __device__ __forceinline__ float row_rescale(float ss, float eps) {
 enum { ROW_NORM = 0, ROW_NORM_TAN = 1, ROW_S8 = 2 };
 
 template <typename T, int C, bool BLOCK, bool VEC, int MODE>
-__global__ void __launch_bounds__(BLOCK ? rownorm_block_threads<T>() : ROWNORM_THREADS, BLOCK ? 1 : 2)
+__global__ void __launch_bounds__(BLOCK ? rownorm_block_threads<T, C>() : ROWNORM_THREADS)
 row_norm_kernel(const RowNormParams p) {
     constexpr int V = RmsVec<T>::N;
     constexpr bool TAN = MODE == ROW_NORM_TAN;
     constexpr int N = MODE == ROW_NORM ? 1 : 2;
-    __shared__ float slots[BLOCK ? 2 * 32 * N : 1];
+    __shared__ __align__(16) float slots[BLOCK ? 2 * 32 * N : 1];
+    if constexpr (BLOCK) clear_slots(slots, 2 * 32 * N);
     const int lane = threadIdx.x & 31, rpw = BLOCK ? 1 : 32 / p.P;
     const RowLane<T, VEC> L{BLOCK ? (int)threadIdx.x : lane & (p.P - 1), BLOCK ? (int)blockDim.x : p.P, p.D};
     const unsigned per_block = BLOCK ? 1u : (ROWNORM_THREADS / 32) * rpw;
@@ -311,13 +348,14 @@ row_norm_kernel(const RowNormParams p) {
 // dx is the gradient of x and of the residual alike.  Every thread keeps the dg terms of its own columns over the rows it
 // walks; a block writes one row of partial sums, and a second kernel adds those up: fixed orders, the same bits each time.
 template <typename T, int C, bool BLOCK, bool VEC, bool TAN>
-__global__ void __launch_bounds__(BLOCK ? rownorm_block_threads<T>() : ROWNORM_BWD_THREADS, BLOCK ? 1 : 3)
+__global__ void __launch_bounds__(BLOCK ? rownorm_block_threads<T, C>() : ROWNORM_THREADS, rownorm_bwd_resident(BLOCK ? rownorm_block_threads<T, C>() : 0, TAN))
 row_norm_bwd_kernel(const RowNormParams p) {
     constexpr int V = RmsVec<T>::N, N = TAN ? 5 : 2;
-    __shared__ float slots[BLOCK ? 2 * 32 * N : 32 * ROWNORM_WARP_CHUNKS * V];
+    __shared__ __align__(16) float slots[BLOCK ? 2 * 32 * N : 32 * V];
+    if constexpr (BLOCK) clear_slots(slots, 2 * 32 * N);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rpw = BLOCK ? 1 : 32 / p.P;
     const RowLane<T, VEC> L{BLOCK ? (int)threadIdx.x : lane & (p.P - 1), BLOCK ? (int)blockDim.x : p.P, p.D};
-    const unsigned per_block = BLOCK ? 1u : (ROWNORM_BWD_THREADS / 32) * rpw;
+    const unsigned per_block = BLOCK ? 1u : (ROWNORM_THREADS / 32) * rpw;
     const float inv_d = 1.0f / (float)p.D;
     unsigned turn = 0;
     uint64_t dg[C][V / 2];
@@ -329,7 +367,8 @@ row_norm_bwd_kernel(const RowNormParams p) {
         const unsigned row = BLOCK ? base : base + warp * rpw + lane / p.P;
         const bool act = BLOCK || row < p.total;
         const unsigned at = act ? row : 0;
-        uint4 hr[C], yr[C], tr[TAN ? C : 1], zr[TAN ? C : 1];   // as loaded: half the registers that bf16 rows would take as fp32
+        // as loaded: half the registers that bf16 rows would take as fp32
+        uint4 hr[C], yr[C], tr[TAN ? C : 1], zr[TAN ? C : 1], vh[C], vt[TAN ? C : 1];
         {
             const T *ph = row_at<const T>(p.in[0], at, p), *py = row_at<const T>(p.in[1], at, p);
 #pragma unroll
@@ -338,6 +377,13 @@ row_norm_bwd_kernel(const RowNormParams p) {
                 const T *pt = row_at<const T>(p.in[3], at, p), *pz = row_at<const T>(p.in[4], at, p);
 #pragma unroll
                 for (int i = 0; i < C; ++i) { tr[i] = L.raw(pt, act, i); zr[i] = L.raw(pz, act, i); }
+            }
+            const T* dh = p.in[2].p ? row_at<const T>(p.in[2], at, p) : nullptr;
+            const T* dth = TAN && p.in[5].p ? row_at<const T>(p.in[5], at, p) : nullptr;
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                vh[i] = L.raw(dh, act && dh, i);
+                if constexpr (TAN) vt[i] = L.raw(dth, act && dth, i);
             }
         }
         auto unpack = [&](int i, uint64_t (&h)[V / 2], uint64_t (&y)[V / 2], uint64_t (&t)[V / 2], uint64_t (&z)[V / 2]) {
@@ -399,15 +445,11 @@ row_norm_bwd_kernel(const RowNormParams p) {
             const uint64_t zh2 = ptx::pack2(zh, zh), jt2 = ptx::pack2(jt, jt);
             T* dx = row_at<T>(p.out[0], at, p);
             T* dtx = TAN ? row_at<T>(p.out[1], at, p) : nullptr;
-            const T* dh = p.in[2].p ? row_at<const T>(p.in[2], at, p) : nullptr;
-            const T* dth = TAN && p.in[5].p ? row_at<const T>(p.in[5], at, p) : nullptr;
 #pragma unroll
             for (int i = 0; i < C; ++i) {
                 uint64_t g[V / 2], ox[V / 2], ot[V / 2], h[V / 2], y[V / 2], t[V / 2], z[V / 2];
-#pragma unroll
-                for (int e = 0; e < V / 2; ++e) ox[e] = ot[e] = 0ull;
-                if (dh) L.load(dh, true, i, ox);
-                if (dth) L.load(dth, true, i, ot);
+                rms_unpack(vh[i], ox);
+                if constexpr (TAN) rms_unpack(vt[i], ot);
                 L.scale(p.g, i, g);
                 keep(hr[i]); keep(yr[i]);
                 if constexpr (TAN) { keep(tr[i]); keep(zr[i]); }
@@ -444,7 +486,7 @@ row_norm_bwd_kernel(const RowNormParams p) {
                 if (L.col(i, e) < p.D) partial[L.col(i, e)] = e & 1 ? b : a;
             }
     } else {
-        for (int w = 0; w < ROWNORM_BWD_THREADS / 32; ++w) {   // the warps one after the other
+        for (int w = 0; w < ROWNORM_THREADS / 32; ++w) {   // the warps one after the other
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < C; ++i)
@@ -460,26 +502,30 @@ row_norm_bwd_kernel(const RowNormParams p) {
                 }
         }
         __syncthreads();
-        for (int j = threadIdx.x; j < p.D; j += ROWNORM_BWD_THREADS) partial[j] = slots[j];
+        for (int j = threadIdx.x; j < p.D; j += ROWNORM_THREADS) partial[j] = slots[j];
     }
 }
 
-// dg[j] = sum over the n partial rows, in a fixed order: a warp takes every 32nd row of 32 columns.  Launched as a programmatic
+// dg[j] = sum over the n partial rows, in a fixed order: 8 columns a block, the rows over 128 threads.  Launched as a programmatic
 // dependent of the kernel above.  n = 0 (no rows at all) gives zeros.
 __global__ void __launch_bounds__(1024) row_norm_dg_kernel(const float* __restrict__ partial, float* __restrict__ dg, int n, int D) {
-    __shared__ float acc[32][33];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
+    __shared__ float acc[32][8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 8 + (lane & 7);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     float v = 0.f;
     if (j < D) {
 #pragma unroll 8
-        for (int b = warp; b < n; b += 32) v += partial[(size_t)b * D + j];
+        for (int b = threadIdx.x >> 3; b < n; b += 128) v += partial[(size_t)b * D + j];
     }
-    acc[warp][lane] = v;
+    v += __shfl_xor_sync(0xffffffffu, v, 8);
+    v += __shfl_xor_sync(0xffffffffu, v, 16);
+    if (lane < 8) acc[warp][lane] = v;
     __syncthreads();
-    v = acc[lane][warp];   // column `warp` of the 32, partial sum `lane`
-    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-    if (lane == 0 && blockIdx.x * 32 + warp < D) dg[blockIdx.x * 32 + warp] = v;
+    if (warp < 8) {   // a column each
+        v = acc[lane][warp];
+        for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+        if (lane == 0 && blockIdx.x * 8 + warp < D) dg[blockIdx.x * 8 + warp] = v;
+    }
 }
 
 }  // namespace tvm_attn

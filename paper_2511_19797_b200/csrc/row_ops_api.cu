@@ -66,31 +66,29 @@ struct RowsCall {
     }
 };
 
-// How a row is split over threads: chunks of 16 bytes, C on each of P lanes of a warp, or of a block of `threads`.
+// How a row is split over threads: chunks of 16 bytes, one on each of P lanes of a warp, or C on each of the `threads` of a block.
 struct RowSplit { int C, P, threads; };
 static RowSplit row_split(int D, int esz) {
     const int chunks = (D * esz + 15) / 16;
-    if (chunks <= 32 * ROWNORM_WARP_CHUNKS) {
-        // four chunks on as few lanes as that takes (a warp has more rows, and fewer steps to add one up)
+    if (chunks <= 32) {
         int P = 1;
-        while (P < 32 && 4 * P < chunks) P *= 2;
-        const int C = (chunks + P - 1) / P;
-        return {C < 2 ? 2 : C, P, 0};
+        while (P < chunks) P *= 2;
+        return {1, P, 0};
     }
-    const int warps = (chunks + 127) / 128;   // three or four chunks a thread
-    return {(chunks + 32 * warps - 1) / (32 * warps), 32 * warps, 32 * warps};
+    const int C = chunks <= 160 ? 1 : chunks <= 1024 ? 2 : 4;
+    const int threads = ((chunks + C - 1) / C + 31) / 32 * 32;
+    return {C, threads, threads};
 }
 
 // launch(C, whether a row has a block) as types, for the split of a call.
 template <typename F>
 static int with_row_split(const RowSplit& s, const F& launch) {
     using std::integral_constant;
-    if (s.threads) return s.C <= 3 ? launch(integral_constant<int, 3>(), std::true_type()) : launch(integral_constant<int, 4>(), std::true_type());
+    if (!s.threads) return launch(integral_constant<int, 1>(), std::false_type());
     switch (s.C) {
-        case 2: return launch(integral_constant<int, 2>(), std::false_type());
-        case 3: return launch(integral_constant<int, 3>(), std::false_type());
-        case 4: return launch(integral_constant<int, 4>(), std::false_type());
-        default: return launch(integral_constant<int, 5>(), std::false_type());
+        case 1: return launch(integral_constant<int, 1>(), std::true_type());
+        case 2: return launch(integral_constant<int, 2>(), std::true_type());
+        default: return launch(integral_constant<int, 4>(), std::true_type());
     }
 }
 
@@ -117,9 +115,9 @@ static int launch_norm(const RowsCall& c, cudaStream_t st) {
     return c.p.dtype == TVM_ATTN_FP32 ? launch_norm<float, MODE>(c, st) : launch_norm<__nv_bfloat16, MODE>(c, st);
 }
 
-static int bwd_blocks(const RowSplit& split, long long rows) {
-    const int per_block = split.threads ? 1 : ROWNORM_BWD_THREADS / 32 * (32 / split.P);
-    return (int)fewer((rows + per_block - 1) / per_block, rownorm_bwd_blocks(split.threads / 32));
+static int bwd_blocks(const RowSplit& split, bool tan, long long rows) {
+    const int per_block = split.threads ? 1 : ROWNORM_THREADS / 32 * (32 / split.P);
+    return (int)fewer((rows + per_block - 1) / per_block, rownorm_bwd_blocks(split.threads, tan));
 }
 
 template <typename T, bool TAN>
@@ -127,10 +125,10 @@ static int launch_norm_bwd(const RowsCall& c, float* dg, cudaStream_t st) {
     const RowSplit split = row_split(c.k.D, sizeof(T));
     RowNormParams k = c.k;
     k.P = split.P;
-    const int blocks = bwd_blocks(split, k.total);
+    const int blocks = bwd_blocks(split, TAN, k.total);
     if (blocks > 0) {
         const int rc = with_row_split(split, [&](auto C, auto block) {
-            const int threads = block() ? split.threads : ROWNORM_BWD_THREADS;
+            const int threads = block() ? split.threads : ROWNORM_THREADS;
             if (c.vec) row_norm_bwd_kernel<T, C(), block(), true, TAN><<<blocks, threads, 0, st>>>(k);
             else row_norm_bwd_kernel<T, C(), block(), false, TAN><<<blocks, threads, 0, st>>>(k);
             g_launches += 1;
@@ -140,7 +138,7 @@ static int launch_norm_bwd(const RowsCall& c, float* dg, cudaStream_t st) {
     }
     if (!dg) return TVM_ATTN_OK;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(k.D + 31) / 32);
+    cfg.gridDim = dim3((unsigned)(k.D + 7) / 8);
     cfg.blockDim = dim3(1024);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -156,7 +154,8 @@ static int launch_norm_bwd(const RowsCall& c, float* dg, cudaStream_t st) {
 
 static size_t norm_bwd_workspace(const tvm_attn_rows_params& p) {
     const RowSplit split = row_split(p.D, p.dtype == TVM_ATTN_FP32 ? 4 : 2);
-    return (size_t)rownorm_bwd_blocks(split.threads / 32) * (size_t)p.D * sizeof(float);
+    const int tan = rownorm_bwd_blocks(split.threads, true), plain = rownorm_bwd_blocks(split.threads, false);
+    return (size_t)(tan > plain ? tan : plain) * (size_t)p.D * sizeof(float);
 }
 
 }  // namespace tvm_attn
