@@ -17,9 +17,9 @@
 
 namespace tvm_attn {
 
-// Rows of a (B, T, D) tensor: element strides between the rows of a batch and between batches.
+// The rows of a (B, T, D) tensor, strides in bytes.
 struct RowsPtr {
-    void* p;
+    char* p;
     long long row, batch;
 };
 
@@ -31,6 +31,7 @@ struct RowNormParams {
     unsigned total, T;
     int D, P;         // P: lanes of a row (all threads of the block where a row has one of its own)
     float eps;
+    bool flat;        // every tensor is one dimension of rows less than 4 GB apart
     bool norm;        // 8-bit rows: of the norm's output (else of x + res itself)
 };
 
@@ -53,62 +54,57 @@ struct RowLane {
     static constexpr int V = RmsVec<T>::N;
     int c, P, D;
     __device__ __forceinline__ int col(int i, int e) const { return VEC ? (c + P * i) * V + e : c + P * (i * V + e); }
-    // A chunk as it lies in memory, zeros behind the row.
+    // A chunk as it lies in memory, zeros behind the row.  `row`: its address at column col(0, 0).
     __device__ __forceinline__ uint4 raw(const T* row, bool act, int i) const {
         uint4 q = make_uint4(0, 0, 0, 0);
         if constexpr (VEC) {
-            if (act && col(i, 0) < D) q = *reinterpret_cast<const uint4*>(row + col(i, 0));
+            if (act && col(i, 0) < D) q = *reinterpret_cast<const uint4*>(row + P * i * V);
         } else {
             uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
             for (int e = 0; e < V; ++e)
                 if (act && col(i, e) < D) {
-                    if constexpr (V == 4) w[e] = __float_as_uint(row[col(i, e)]);
-                    else w[e / 2] |= (uint32_t)__bfloat16_as_ushort(row[col(i, e)]) << (16 * (e & 1));
+                    const T x = row[P * (i * V + e)];
+                    if constexpr (V == 4) w[e] = __float_as_uint(x);
+                    else w[e / 2] |= (uint32_t)__bfloat16_as_ushort(x) << (16 * (e & 1));
                 }
             q = make_uint4(w[0], w[1], w[2], w[3]);
         }
         return q;
     }
-    __device__ __forceinline__ void load(const T* row, bool act, int i, uint64_t (&v)[V / 2]) const { rms_unpack(raw(row, act, i), v); }
     __device__ __forceinline__ void store(T* row, int i, const uint64_t (&v)[V / 2]) const {
         if constexpr (VEC) {
-            if (col(i, 0) < D) rms_store(row + col(i, 0), v);
+            if (col(i, 0) < D) rms_store(row + P * i * V, v);
         } else {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 float a, b;
                 ptx::unpack2(v[e / 2], a, b);
-                if (col(i, e) < D) row[col(i, e)] = (T)(e & 1 ? b : a);
+                if (col(i, e) < D) row[P * (i * V + e)] = (T)(e & 1 ? b : a);
             }
         }
     }
     // The scale's elements for a chunk: 1 where there is no scale, 0 behind the row.
     __device__ __forceinline__ void scale(const float* g, int i, uint64_t (&v)[V / 2]) const {
-        if (!g) {
 #pragma unroll
-            for (int e = 0; e < V / 2; ++e) v[e] = ptx::pack2(1.f, 1.f);
-        } else if constexpr (VEC) {
-#pragma unroll
-            for (int e = 0; e < V / 2; e += 2) {
-                float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (col(i, 0) < D) q = __ldg(reinterpret_cast<const float4*>(g + col(i, 2 * e)));
-                v[e] = ptx::pack2(q.x, q.y);
-                v[e + 1] = ptx::pack2(q.z, q.w);
+        for (int e = 0; e < V; e += 2) {
+            float a = 1.f, b = 1.f;
+            if (g) {
+                a = col(i, e) < D ? __ldg(g + col(i, e)) : 0.f;
+                b = col(i, e + 1) < D ? __ldg(g + col(i, e + 1)) : 0.f;
             }
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; e += 2) v[e / 2] = ptx::pack2(col(i, e) < D ? __ldg(g + col(i, e)) : 0.f, col(i, e + 1) < D ? __ldg(g + col(i, e + 1)) : 0.f);
+            v[e / 2] = ptx::pack2(a, b);
         }
     }
+    // Address of a tensor's row 0 at the lane's first column, and from it that of row `row`: one instruction where the rows are
+    // one dimension.  `size`: of an element.
+    __device__ __forceinline__ char* base(const RowsPtr& t, int size) const { return t.p + (size_t)col(0, 0) * size; }
+    __device__ __forceinline__ static char* at(char* base, const RowsPtr& t, unsigned row, const RowNormParams& p) {
+        if (p.flat) return base + (size_t)row * (unsigned)t.row;
+        const unsigned b = row / p.T;
+        return base + (size_t)b * (size_t)t.batch + (size_t)(row - b * p.T) * (size_t)t.row;
+    }
 };
-
-template <typename T>
-__device__ __forceinline__ T* row_at(const RowsPtr& t, unsigned row, const RowNormParams& p) {
-    if (p.T == p.total) return static_cast<T*>(t.p) + (size_t)row * (size_t)t.row;
-    const unsigned b = row / p.T;
-    return static_cast<T*>(t.p) + (size_t)b * (size_t)t.batch + (size_t)(row - b * p.T) * (size_t)t.row;
-}
 
 __device__ __forceinline__ float max_nan(float a, float b) {   // a NaN on either side stays
     float r;
@@ -116,59 +112,82 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // a NaN on eithe
     return r;
 }
 
-// N sums over a row (the last one a maximum with MAX), returned to all its lanes, the same bits on each.  In a block with one row
-// the lanes of a warp halve the values among them with every step (8 shuffles for 5 values, not 25), a lane writes each to `slot`, 32 N
-// floats of shared memory that are zero behind the block's warps, and all threads add the warps' parts up in the same order.  Two
-// slots are used in turn, so that one barrier a reduction is enough.
-template <int N, bool MAX, bool BLOCK>
-__device__ __forceinline__ void row_reduce(float (&v)[N], int P, float* slot) {
-    if constexpr (!BLOCK) {
+// The sums of N values (the last one a maximum with MAX, where N = 2) over P lanes, each on some of them: the lanes halve the
+// values among them with every step.  5 values: by the three highest bits of the lane's place, 000, 001, 010, 100 and 101 hold values
+// 0 to 4, the others nothing; 2 values: by the highest bit.
+template <int N, bool MAX>
+__device__ __forceinline__ float row_scatter(const float (&v)[N], int P, int lane) {
+    float part[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) part[k] = v[k];
+    int off = P >> 1, n = N;
+    const bool last = lane & off;
+#pragma unroll
+    for (int step = 0; step < 3; ++step) {   // 5 -> 3 -> 2 -> 1
+        if (n == 1) break;
+        const bool high = lane & off;
+        const int half = (n + 1) / 2;
+#pragma unroll
+        for (int k = 0; k < (N + 1) / 2; ++k) {
+            if (k >= half) continue;
+            const float lo = part[k], hi = k + half < n ? part[k + half < N ? k + half : 0] : 0.f;
+            const float keep = high ? hi : lo, w = __shfl_xor_sync(0xffffffffu, high ? lo : hi, off);
+            part[k] = MAX && high ? max_nan(keep, w) : keep + w;
+        }
+        n = half;
+        off >>= 1;
+    }
+    for (; off > 0; off >>= 1) {
+        const float w = __shfl_xor_sync(0xffffffffu, part[0], off);
+        part[0] = MAX && last ? max_nan(part[0], w) : part[0] + w;
+    }
+    return part[0];
+}
+// The same, all sums on all lanes, the same bits on each.
+template <int N, bool MAX>
+__device__ __forceinline__ void row_all(float (&v)[N], int P, int lane) {
+    if (N == 1 || P < 8) {
         for (int off = P >> 1; off > 0; off >>= 1)
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 const float w = __shfl_xor_sync(0xffffffffu, v[k], off);
                 v[k] = MAX && k == N - 1 ? max_nan(v[k], w) : v[k] + w;
             }
+        return;
+    }
+    const float part = row_scatter<N, MAX>(v, P, lane);
+    const int first = lane & ~(P - 1), bit = N == 2 ? P >> 1 : P >> 3;
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, part, first + (k < 3 ? k : k + 1) * bit);
+}
+// The same for a row of a warp's lanes or, with BLOCK, of all threads of a block: `slot`, 32 N floats of shared memory, zeros behind
+// the block's warps.  Two slots are used in turn, so that one barrier a reduction is enough.
+template <int N, bool MAX, bool BLOCK>
+__device__ __forceinline__ void row_reduce(float (&v)[N], int P, float* slot) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if constexpr (!BLOCK) {
+        row_all<N, MAX>(v, P, lane);
     } else {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-        float part[N];
-#pragma unroll
-        for (int k = 0; k < N; ++k) part[k] = v[k];
-        int id = 0, left = N;   // the first of the `left` values that this lane still holds (padding among them)
-        bool real = true;
-        int n = N;
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) {
-            const bool high = lane & off;
-            if (n > 1) {
-                const int half = (n + 1) / 2;
-#pragma unroll
-                for (int k = 0; k < (N + 1) / 2; ++k) {
-                    if (k >= half) continue;
-                    const float lo = part[k], hi = k + half < n ? part[k + half < N ? k + half : 0] : 0.f;
-                    const float keep = high ? hi : lo, w = __shfl_xor_sync(0xffffffffu, high ? lo : hi, off);
-                    part[k] = MAX && high ? max_nan(keep, w) : keep + w;   // (MAX: N = 2, the high lanes have the maximum)
-                }
-                id += high ? half : 0;
-                left = high ? left - half : left < half ? left : half;
-                real = real && left > 0;
-                n = half;
-            } else {
-                const float w = __shfl_xor_sync(0xffffffffu, part[0], off);
-                part[0] = MAX && id == N - 1 ? max_nan(part[0], w) : part[0] + w;
-            }
-        }
-        constexpr int SAME = N == 1 ? 31 : N == 2 ? 15 : 3;   // lanes that differ in these bits hold the same value
-        if ((lane & SAME) == 0 && real) slot[32 * id + warp] = part[0];
+        const float part = row_scatter<N, MAX>(v, 32, lane);
+        const int place = lane >> (N == 1 ? 5 : N == 2 ? 4 : 2), id = N == 5 && place > 2 ? place - 1 : place;
+        if ((lane & (N == 1 ? 31 : N == 2 ? 15 : 3)) == 0 && (N < 5 || (place != 3 && place < 6))) slot[32 * id + warp] = part;
         __syncthreads();
+        if (blockDim.x <= 256) {   // the parts of up to 8 warps, by every thread
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            float sum = 0.f;
-            for (int w = 0; w < warps; w += 4) {
-                const float4 q = *reinterpret_cast<const float4*>(slot + 32 * k + w);
-                sum = MAX && k == N - 1 ? max_nan(sum, max_nan(max_nan(q.x, q.y), max_nan(q.z, q.w))) : sum + ((q.x + q.y) + (q.z + q.w));
+            for (int k = 0; k < N; ++k) {
+                const float4 q = *reinterpret_cast<const float4*>(slot + 32 * k);
+                v[k] = MAX && k == N - 1 ? max_nan(max_nan(q.x, q.y), max_nan(q.z, q.w)) : (q.x + q.y) + (q.z + q.w);
             }
-            v[k] = sum;   // (the maximum is one of magnitudes)
+            if (blockDim.x > 128)
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const float4 q = *reinterpret_cast<const float4*>(slot + 32 * k + 4);
+                    v[k] = MAX && k == N - 1 ? max_nan(v[k], max_nan(max_nan(q.x, q.y), max_nan(q.z, q.w))) : v[k] + ((q.x + q.y) + (q.z + q.w));
+                }
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = slot[32 * k + lane];   // (a maximum is one of magnitudes)
+            row_all<N, MAX>(v, 32, lane);
         }
     }
 }
@@ -191,149 +210,165 @@ enum { ROW_NORM = 0, ROW_NORM_TAN = 1, ROW_S8 = 2 };
 template <typename T, int C, bool BLOCK, bool VEC, int MODE>
 __global__ void __launch_bounds__(BLOCK ? rownorm_block_threads<T, C>() : ROWNORM_THREADS)
 row_norm_kernel(const RowNormParams p) {
-    constexpr int V = RmsVec<T>::N;
+    constexpr int V = RmsVec<T>::N, E = (int)sizeof(T);
     constexpr bool TAN = MODE == ROW_NORM_TAN;
     constexpr int N = MODE == ROW_NORM ? 1 : 2;
-    __shared__ __align__(16) float slots[BLOCK ? 2 * 32 * N : 1];
+    __shared__ __align__(16) float slots[BLOCK ? 2 * 32 * N : 4];
     if constexpr (BLOCK) clear_slots(slots, 2 * 32 * N);
     const int lane = threadIdx.x & 31, rpw = BLOCK ? 1 : 32 / p.P;
-    const RowLane<T, VEC> L{BLOCK ? (int)threadIdx.x : lane & (p.P - 1), BLOCK ? (int)blockDim.x : p.P, p.D};
+    using Lane = RowLane<T, VEC>;
+    const Lane L{BLOCK ? (int)threadIdx.x : lane & (p.P - 1), BLOCK ? (int)blockDim.x : p.P, p.D};
     const unsigned per_block = BLOCK ? 1u : (ROWNORM_THREADS / 32) * rpw;
     const float inv_d = 1.0f / (float)p.D;
+    char *x0 = L.base(p.in[0], E), *r0 = L.base(p.in[1], E), *tx0 = L.base(p.in[2], E), *tr0 = L.base(p.in[3], E);
+    char *y0 = L.base(p.out[0], MODE == ROW_S8 ? 1 : E), *h0 = L.base(p.out[1], E), *ty0 = L.base(p.out[2], E), *th0 = L.base(p.out[3], E);
+    const bool res = p.in[1].p, tres = TAN && p.in[3].p;
+    uint64_t g[C][V / 2];   // the same columns for every row
+#pragma unroll
+    for (int i = 0; i < C; ++i) L.scale(p.g, i, g[i]);
     unsigned turn = 0;
-    auto slot = [&]() { return slots + (BLOCK ? (turn++ & 1u) * 32 * N : 0); };
     for (unsigned base = blockIdx.x * per_block; base < p.total; base += gridDim.x * per_block) {
         const unsigned row = BLOCK ? base : base + (threadIdx.x >> 5) * rpw + lane / p.P;
         const bool act = BLOCK || row < p.total;
         const unsigned at = act ? row : 0;
         uint64_t h[C][V / 2], t[TAN ? C : 1][V / 2];
         {
-            const T* x = row_at<const T>(p.in[0], at, p);
+            const T* x = reinterpret_cast<const T*>(Lane::at(x0, p.in[0], at, p));
+            uint4 a[C], b[C], c[TAN ? C : 1], d[TAN ? C : 1];
 #pragma unroll
-            for (int i = 0; i < C; ++i) L.load(x, act, i, h[i]);
-            if constexpr (TAN) {
-                const T* tx = row_at<const T>(p.in[2], at, p);
+            for (int i = 0; i < C; ++i) a[i] = L.raw(x, act, i);
+            if (res) {
+                const T* r = reinterpret_cast<const T*>(Lane::at(r0, p.in[1], at, p));
 #pragma unroll
-                for (int i = 0; i < C; ++i) L.load(tx, act, i, t[i]);
+                for (int i = 0; i < C; ++i) b[i] = L.raw(r, act, i);
             }
-            if (p.in[1].p) {
-                const T* res = row_at<const T>(p.in[1], at, p);
+            if constexpr (TAN) {
+                const T* tx = reinterpret_cast<const T*>(Lane::at(tx0, p.in[2], at, p));
+#pragma unroll
+                for (int i = 0; i < C; ++i) c[i] = L.raw(tx, act, i);
+                if (tres) {
+                    const T* tr = reinterpret_cast<const T*>(Lane::at(tr0, p.in[3], at, p));
+#pragma unroll
+                    for (int i = 0; i < C; ++i) d[i] = L.raw(tr, act, i);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                rms_unpack(a[i], h[i]);
+                if constexpr (TAN) rms_unpack(c[i], t[i]);
+            }
+            if (res) {
+                T* to = reinterpret_cast<T*>(Lane::at(h0, p.out[1], at, p));
 #pragma unroll
                 for (int i = 0; i < C; ++i) {
                     uint64_t w[V / 2];
-                    L.load(res, act, i, w);
+                    rms_unpack(b[i], w);
 #pragma unroll
                     for (int e = 0; e < V / 2; ++e) h[i][e] = ptx::add2(h[i][e], w[e]);
+                    if (act) L.store(to, i, h[i]);
                 }
             }
             if constexpr (TAN)
-                if (p.in[3].p) {
-                    const T* tres = row_at<const T>(p.in[3], at, p);
+                if (tres) {
+                    T* to = reinterpret_cast<T*>(Lane::at(th0, p.out[3], at, p));
 #pragma unroll
                     for (int i = 0; i < C; ++i) {
                         uint64_t w[V / 2];
-                        L.load(tres, act, i, w);
+                        rms_unpack(d[i], w);
 #pragma unroll
                         for (int e = 0; e < V / 2; ++e) t[i][e] = ptx::add2(t[i][e], w[e]);
+                        if (act) L.store(to, i, t[i]);
                     }
                 }
         }
-        if (p.out[1].p && act) {
-            T* to = row_at<T>(p.out[1], at, p);
-#pragma unroll
-            for (int i = 0; i < C; ++i) L.store(to, i, h[i]);
-        }
-        if constexpr (TAN)
-            if (p.out[3].p && act) {
-                T* to = row_at<T>(p.out[3], at, p);
-#pragma unroll
-                for (int i = 0; i < C; ++i) L.store(to, i, t[i]);
-            }
-        // sums[0] = h . h, sums[1] = h . th or max |g h|; elements times `pre` in the first two
+        // sums[0] = h . h, sums[1] = h . th or max |g h|; h times `pre` in the first two
         float sums[N], pre = 1.f;
-        auto sum_up = [&]() {
+        auto sum_up = [&](bool scaled) {
             const uint64_t pre2 = ptx::pack2(pre, pre);
             uint64_t ss2 = 0ull, s2 = 0ull;
             float top = 0.f;
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                uint64_t g[V / 2];
-                if constexpr (MODE == ROW_S8) L.scale(p.g, i, g);
+            for (int i = 0; i < C; ++i)
 #pragma unroll
                 for (int e = 0; e < V / 2; ++e) {
-                    const uint64_t x = ptx::mul2(h[i][e], pre2);
-                    ss2 = ptx::fma2(x, x, ss2);
+                    const uint64_t x = scaled ? ptx::mul2(h[i][e], pre2) : h[i][e];
+                    if (MODE != ROW_S8 || p.norm) ss2 = ptx::fma2(x, x, ss2);
                     if constexpr (TAN) s2 = ptx::fma2(x, t[i][e], s2);
                     if constexpr (MODE == ROW_S8) {
                         float a, b;
-                        ptx::unpack2(ptx::mul2(h[i][e], g[e]), a, b);
+                        ptx::unpack2(ptx::mul2(h[i][e], g[i][e]), a, b);
                         top = max_nan(top, max_nan(fabsf(a), fabsf(b)));
                     }
                 }
-            }
             sums[0] = rms_hsum(ss2);
             if constexpr (N > 1) sums[N - 1] = MODE == ROW_S8 ? top : rms_hsum(s2);
-            row_reduce<N, MODE == ROW_S8, BLOCK>(sums, p.P, slot());
+            row_reduce<N, MODE == ROW_S8, BLOCK>(sums, p.P, slots + (BLOCK ? (turn++ & 1u) * 32 * N : 0));
         };
-        sum_up();
+        sum_up(false);
         const float again = row_rescale(sums[0], p.eps);
         if (BLOCK ? again != 0.f : __any_sync(0xffffffffu, again != 0.f)) {   // (the rows of the warp that need none keep pre = 1)
             pre = again != 0.f ? again : 1.f;
-            sum_up();
+            sum_up(true);
         }
-        const float root = 1.0f / sqrtf(sums[0] * inv_d + p.eps * pre * pre);   // 1 / (r pre)
+        const float root = rsqrtf(sums[0] * inv_d + p.eps * pre * pre);   // 1 / (r pre)
         const float inv = root * pre;
         if constexpr (MODE == ROW_S8) {
-            // scaled up first where 127 / max would leave the range
+            // scaled up first where 127 / max would leave the range; zeros where the maximum is not finite
             const float top = sums[N - 1], up = top < 0x1p-100f ? 0x1p100f : 1.f;
-            const float k = top > 0.f || top != top ? 127.f / (top * up) : 0.f;
+            const bool fine = top <= 3.4028235e38f && top > 0.f;
+            const float k = fine ? 127.f / (top * up) : 0.f;
             if (act) {
                 if (L.c == 0) p.aux[row] = top * (p.norm ? inv : 1.f) / 127.f;
-                int8_t* to = row_at<int8_t>(p.out[0], at, p);
+                int8_t* to = reinterpret_cast<int8_t*>(Lane::at(y0, p.out[0], at, p));
+                const uint64_t up2 = ptx::pack2(up, up), k2 = ptx::pack2(k, k), round2 = ptx::pack2(12582912.f, 12582912.f);   // 1.5 2^23
 #pragma unroll
                 for (int i = 0; i < C; ++i) {
-                    uint64_t g[V / 2];
-                    L.scale(p.g, i, g);
-                    int q[V];
+                    // 1.5 2^23 + x, |x| <= 127, rounds x to the nearest whole number (even on ties), whose 8 bits are the sum's lowest
+                    uint32_t q[V];
 #pragma unroll
                     for (int e = 0; e < V / 2; ++e) {
+                        uint64_t v = ptx::mul2(h[i][e], g[i][e]);
+                        if (up != 1.f) v = ptx::mul2(v, up2);
                         float a, b;
-                        ptx::unpack2(ptx::mul2(h[i][e], g[e]), a, b);
-                        q[2 * e] = __float2int_rn(a * up * k);   // (not a number: 0)
-                        q[2 * e + 1] = __float2int_rn(b * up * k);
+                        ptx::unpack2(ptx::add2(ptx::mul2(v, k2), round2), a, b);
+                        q[2 * e] = __float_as_uint(a);
+                        q[2 * e + 1] = __float_as_uint(b);
                     }
                     if constexpr (VEC) {
                         uint32_t w[V / 4];
 #pragma unroll
-                        for (int e = 0; e < V / 4; ++e)
+                        for (int e = 0; e < V / 4; ++e) {
                             w[e] = __byte_perm(__byte_perm(q[4 * e], q[4 * e + 1], 0x0040), __byte_perm(q[4 * e + 2], q[4 * e + 3], 0x0040), 0x5410);
+                            if (!fine) w[e] = 0;
+                        }
                         if (L.col(i, 0) < p.D) {
-                            if constexpr (V == 8) *reinterpret_cast<uint2*>(to + L.col(i, 0)) = make_uint2(w[0], w[V / 4 - 1]);
-                            else *reinterpret_cast<uint32_t*>(to + L.col(i, 0)) = w[0];
+                            if constexpr (V == 8) *reinterpret_cast<uint2*>(to + L.P * i * V) = make_uint2(w[0], w[V / 4 - 1]);
+                            else *reinterpret_cast<uint32_t*>(to + L.P * i * V) = w[0];
                         }
                     } else {
 #pragma unroll
                         for (int e = 0; e < V; ++e)
-                            if (L.col(i, e) < p.D) to[L.col(i, e)] = (int8_t)q[e];
+                            if (L.col(i, e) < p.D) to[L.P * (i * V + e)] = fine ? (int8_t)q[e] : (int8_t)0;
                     }
                 }
             }
         } else if (act) {
-            const float m = TAN ? sums[N - 1] * root * root * inv_d : 0.f;   // (u . th) / (D r pre) = (u . th) root / D
-            const uint64_t inv2 = ptx::pack2(inv, inv), nm2 = ptx::pack2(-m * pre, -m * pre);
-            T* y = row_at<T>(p.out[0], at, p);
-            T* ty = TAN ? row_at<T>(p.out[2], at, p) : nullptr;
+            const float m = TAN ? sums[N - 1] * root * root * inv_d * pre : 0.f;   // (u . th) / (D r): th . h pre is known
+            const uint64_t inv2 = ptx::pack2(inv, inv), nm2 = ptx::pack2(-m, -m);
+            T* y = reinterpret_cast<T*>(Lane::at(y0, p.out[0], at, p));
+            T* ty = TAN ? reinterpret_cast<T*>(Lane::at(ty0, p.out[2], at, p)) : nullptr;
 #pragma unroll
             for (int i = 0; i < C; ++i) {
-                uint64_t g[V / 2], o[V / 2];
-                L.scale(p.g, i, g);
+                uint64_t o[V / 2], u[V / 2];
 #pragma unroll
-                for (int e = 0; e < V / 2; ++e) o[e] = ptx::mul2(g[e], ptx::mul2(h[i][e], inv2));
+                for (int e = 0; e < V / 2; ++e) {
+                    u[e] = ptx::mul2(h[i][e], inv2);
+                    o[e] = ptx::mul2(g[i][e], u[e]);
+                }
                 L.store(y, i, o);
                 if constexpr (TAN) {
 #pragma unroll
-                    for (int e = 0; e < V / 2; ++e)
-                        o[e] = ptx::mul2(g[e], ptx::fma2(ptx::mul2(h[i][e], inv2), nm2, ptx::mul2(t[i][e], inv2)));
+                    for (int e = 0; e < V / 2; ++e) o[e] = ptx::mul2(g[i][e], ptx::fma2(u[e], nm2, ptx::mul2(t[i][e], inv2)));
                     L.store(ty, i, o);
                 }
             }
@@ -350,19 +385,25 @@ row_norm_kernel(const RowNormParams p) {
 template <typename T, int C, bool BLOCK, bool VEC, bool TAN>
 __global__ void __launch_bounds__(BLOCK ? rownorm_block_threads<T, C>() : ROWNORM_THREADS, rownorm_bwd_resident(BLOCK ? rownorm_block_threads<T, C>() : 0, TAN))
 row_norm_bwd_kernel(const RowNormParams p) {
-    constexpr int V = RmsVec<T>::N, N = TAN ? 5 : 2;
+    constexpr int V = RmsVec<T>::N, N = TAN ? 5 : 2, E = (int)sizeof(T);
     __shared__ __align__(16) float slots[BLOCK ? 2 * 32 * N : 32 * V];
     if constexpr (BLOCK) clear_slots(slots, 2 * 32 * N);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rpw = BLOCK ? 1 : 32 / p.P;
-    const RowLane<T, VEC> L{BLOCK ? (int)threadIdx.x : lane & (p.P - 1), BLOCK ? (int)blockDim.x : p.P, p.D};
+    using Lane = RowLane<T, VEC>;
+    const Lane L{BLOCK ? (int)threadIdx.x : lane & (p.P - 1), BLOCK ? (int)blockDim.x : p.P, p.D};
     const unsigned per_block = BLOCK ? 1u : (ROWNORM_THREADS / 32) * rpw;
     const float inv_d = 1.0f / (float)p.D;
-    unsigned turn = 0;
-    uint64_t dg[C][V / 2];
+    char *h0 = L.base(p.in[0], E), *y0 = L.base(p.in[1], E), *vh0 = L.base(p.in[2], E), *t0 = L.base(p.in[3], E), *z0 = L.base(p.in[4], E), *vt0 = L.base(p.in[5], E);
+    char *dx0 = L.base(p.out[0], E), *dt0 = L.base(p.out[1], E);
+    const bool dh = p.in[2].p, dth = TAN && p.in[5].p;
+    uint64_t g[C][V / 2], dg[C][V / 2];
 #pragma unroll
-    for (int i = 0; i < C; ++i)
+    for (int i = 0; i < C; ++i) {
+        L.scale(p.g, i, g[i]);
 #pragma unroll
         for (int e = 0; e < V / 2; ++e) dg[i][e] = 0ull;
+    }
+    unsigned turn = 0;
     for (unsigned base = blockIdx.x * per_block; base < p.total; base += gridDim.x * per_block) {
         const unsigned row = BLOCK ? base : base + warp * rpw + lane / p.P;
         const bool act = BLOCK || row < p.total;
@@ -370,21 +411,15 @@ row_norm_bwd_kernel(const RowNormParams p) {
         // as loaded: half the registers that bf16 rows would take as fp32
         uint4 hr[C], yr[C], tr[TAN ? C : 1], zr[TAN ? C : 1], vh[C], vt[TAN ? C : 1];
         {
-            const T *ph = row_at<const T>(p.in[0], at, p), *py = row_at<const T>(p.in[1], at, p);
+            auto load = [&](uint4* to, char* base, int k, bool there) {
+                const T* from = reinterpret_cast<const T*>(Lane::at(base, p.in[k], at, p));
 #pragma unroll
-            for (int i = 0; i < C; ++i) { hr[i] = L.raw(ph, act, i); yr[i] = L.raw(py, act, i); }
-            if constexpr (TAN) {
-                const T *pt = row_at<const T>(p.in[3], at, p), *pz = row_at<const T>(p.in[4], at, p);
-#pragma unroll
-                for (int i = 0; i < C; ++i) { tr[i] = L.raw(pt, act, i); zr[i] = L.raw(pz, act, i); }
-            }
-            const T* dh = p.in[2].p ? row_at<const T>(p.in[2], at, p) : nullptr;
-            const T* dth = TAN && p.in[5].p ? row_at<const T>(p.in[5], at, p) : nullptr;
-#pragma unroll
-            for (int i = 0; i < C; ++i) {
-                vh[i] = L.raw(dh, act && dh, i);
-                if constexpr (TAN) vt[i] = L.raw(dth, act && dth, i);
-            }
+                for (int i = 0; i < C; ++i) to[i] = L.raw(from, act && there, i);
+            };
+            load(hr, h0, 0, true);
+            load(yr, y0, 1, true);
+            if constexpr (TAN) { load(tr, t0, 3, true); load(zr, z0, 4, true); load(vt, vt0, 5, dth); }
+            load(vh, vh0, 2, dh);
         }
         auto unpack = [&](int i, uint64_t (&h)[V / 2], uint64_t (&y)[V / 2], uint64_t (&t)[V / 2], uint64_t (&z)[V / 2]) {
             rms_unpack(hr[i], h);
@@ -395,23 +430,22 @@ row_norm_bwd_kernel(const RowNormParams p) {
         auto keep = [](uint4& q) { asm volatile("" : "+r"(q.x), "+r"(q.y), "+r"(q.z), "+r"(q.w)); };
         // h.h, a.h, then with tangents h.th, b.h, b.th; h times `pre`
         float s[N], pre = 1.f;
-        auto sum_up = [&]() {
+        auto sum_up = [&](bool scaled) {
             const uint64_t pre2 = ptx::pack2(pre, pre);
             uint64_t acc[N];
 #pragma unroll
             for (int k = 0; k < N; ++k) acc[k] = 0ull;
 #pragma unroll
             for (int i = 0; i < C; ++i) {
-                uint64_t g[V / 2], h[V / 2], y[V / 2], t[V / 2], z[V / 2];
-                L.scale(p.g, i, g);
+                uint64_t h[V / 2], y[V / 2], t[V / 2], z[V / 2];
                 unpack(i, h, y, t, z);
 #pragma unroll
                 for (int e = 0; e < V / 2; ++e) {
-                    const uint64_t x = ptx::mul2(h[e], pre2);
+                    const uint64_t x = scaled ? ptx::mul2(h[e], pre2) : h[e];
                     acc[0] = ptx::fma2(x, x, acc[0]);
-                    acc[1] = ptx::fma2(ptx::mul2(g[e], y[e]), x, acc[1]);
+                    acc[1] = ptx::fma2(ptx::mul2(g[i][e], y[e]), x, acc[1]);
                     if constexpr (TAN) {
-                        const uint64_t b = ptx::mul2(g[e], z[e]);
+                        const uint64_t b = ptx::mul2(g[i][e], z[e]);
                         acc[2] = ptx::fma2(x, t[e], acc[2]);
                         acc[3] = ptx::fma2(b, x, acc[3]);
                         acc[4] = ptx::fma2(b, t[e], acc[4]);
@@ -422,13 +456,13 @@ row_norm_bwd_kernel(const RowNormParams p) {
             for (int k = 0; k < N; ++k) s[k] = rms_hsum(acc[k]);
             row_reduce<N, false, BLOCK>(s, p.P, slots + (BLOCK ? (turn++ & 1u) * 32 * N : 0));
         };
-        sum_up();
+        sum_up(false);
         const float again = row_rescale(s[0], p.eps);
         if (BLOCK ? again != 0.f : __any_sync(0xffffffffu, again != 0.f)) {
             pre = again != 0.f ? again : 1.f;
-            sum_up();
+            sum_up(true);
         }
-        const float root = 1.0f / sqrtf(s[0] * inv_d + p.eps * pre * pre), inv = root * pre;
+        const float root = rsqrtf(s[0] * inv_d + p.eps * pre * pre), inv = root * pre;
         const float au = s[1] * root;
         // dx = inv a + kh u + kb b + kt th, dtx = inv b + zh u;  u = h inv
         float kh = -inv * au * inv_d, kb = 0.f, kt = 0.f, zh = 0.f, jt = 0.f;
@@ -443,29 +477,27 @@ row_norm_bwd_kernel(const RowNormParams p) {
         if (act) {
             const uint64_t inv2 = ptx::pack2(inv, inv), kh2 = ptx::pack2(kh, kh), kb2 = ptx::pack2(kb, kb), kt2 = ptx::pack2(kt, kt);
             const uint64_t zh2 = ptx::pack2(zh, zh), jt2 = ptx::pack2(jt, jt);
-            T* dx = row_at<T>(p.out[0], at, p);
-            T* dtx = TAN ? row_at<T>(p.out[1], at, p) : nullptr;
+            T* dx = reinterpret_cast<T*>(Lane::at(dx0, p.out[0], at, p));
+            T* dtx = TAN ? reinterpret_cast<T*>(Lane::at(dt0, p.out[1], at, p)) : nullptr;
 #pragma unroll
             for (int i = 0; i < C; ++i) {
-                uint64_t g[V / 2], ox[V / 2], ot[V / 2], h[V / 2], y[V / 2], t[V / 2], z[V / 2];
+                uint64_t ox[V / 2], ot[V / 2], h[V / 2], y[V / 2], t[V / 2], z[V / 2];
                 rms_unpack(vh[i], ox);
                 if constexpr (TAN) rms_unpack(vt[i], ot);
-                L.scale(p.g, i, g);
                 keep(hr[i]); keep(yr[i]);
                 if constexpr (TAN) { keep(tr[i]); keep(zr[i]); }
                 unpack(i, h, y, t, z);
 #pragma unroll
                 for (int e = 0; e < V / 2; ++e) {
-                    const uint64_t u = ptx::mul2(h[e], inv2), a = ptx::mul2(g[e], y[e]);
-                    ox[e] = ptx::add2(ptx::fma2(a, inv2, ptx::mul2(u, kh2)), ox[e]);
-                    uint64_t term = ptx::mul2(y[e], u);
+                    const uint64_t u = ptx::mul2(h[e], inv2), a = ptx::mul2(g[i][e], y[e]);
+                    ox[e] = ptx::fma2(a, inv2, ptx::fma2(u, kh2, ox[e]));
+                    dg[i][e] = ptx::fma2(y[e], u, dg[i][e]);
                     if constexpr (TAN) {
-                        const uint64_t b = ptx::mul2(g[e], z[e]);
+                        const uint64_t b = ptx::mul2(g[i][e], z[e]);
                         ox[e] = ptx::fma2(b, kb2, ptx::fma2(t[e], kt2, ox[e]));
-                        ot[e] = ptx::add2(ptx::fma2(b, inv2, ptx::mul2(u, zh2)), ot[e]);
-                        term = ptx::fma2(z[e], ptx::fma2(t[e], inv2, ptx::mul2(u, jt2)), term);
+                        ot[e] = ptx::fma2(b, inv2, ptx::fma2(u, zh2, ot[e]));
+                        dg[i][e] = ptx::fma2(z[e], ptx::fma2(t[e], inv2, ptx::mul2(u, jt2)), dg[i][e]);
                     }
-                    dg[i][e] = ptx::add2(dg[i][e], term);
                 }
                 L.store(dx, i, ox);
                 if constexpr (TAN) L.store(dtx, i, ot);

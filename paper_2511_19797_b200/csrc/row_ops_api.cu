@@ -38,6 +38,7 @@ struct RowsCall {
         esz = q.dtype == TVM_ATTN_FP32 ? 4 : 2;
         k.total = (unsigned)((long long)q.B * q.T);
         k.T = k.total;   // one dimension of rows, until a tensor needs two
+        k.flat = true;
         k.D = q.D;
         k.eps = q.eps;
         vec = q.D * esz % 16 == 0;
@@ -54,8 +55,9 @@ struct RowsCall {
         if (p.B <= 1) batch = row * p.T;
         if (k.total <= 1) row = batch = p.D;
         if (row < p.D || batch < p.D || row > (1LL << 40) || batch > (1LL << 40) || reinterpret_cast<uintptr_t>(t->ptr) % size) { ok = false; return; }
-        *to = {t->ptr, row, batch};
-        if (p.T > 1 && batch != row * p.T) k.T = (unsigned)p.T;
+        *to = {static_cast<char*>(t->ptr), row * size, batch * size};
+        if (p.T > 1 && batch != row * p.T) { k.T = (unsigned)p.T; k.flat = false; }
+        if (row * size >= 1LL << 32) k.flat = false;
         const long long unit = eight ? 8 : 16;
         vec = vec && reinterpret_cast<uintptr_t>(t->ptr) % unit == 0 && row * size % unit == 0 && batch * size % unit == 0;
     }
@@ -94,19 +96,37 @@ static int with_row_split(const RowSplit& s, const F& launch) {
 
 static unsigned fewer(long long a, long long b) { return (unsigned)(a < b ? a : b); }
 
+// Blocks of `threads` that the device holds at a time, looked up once per thread, context and block size.
+template <auto KERN>
+static long long resident_blocks(const DeviceFacts& dev, int threads) {
+    thread_local unsigned long long ctx = 0;
+    thread_local int known = 0, blocks = 0;
+    if (ctx != dev.ctx || known != threads) {
+        int n = 0;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, KERN, threads, 0) != cudaSuccess || n < 1) { cudaGetLastError(); return 0; }
+        ctx = dev.ctx; known = threads; blocks = n;
+    }
+    return (long long)blocks * dev.sms;
+}
+
 template <typename T, int MODE>
 static int launch_norm(const RowsCall& c, cudaStream_t st) {
+    const DeviceFacts* dev = device_facts();
+    if (!dev) return TVM_ATTN_CUDA_ERROR;
     const RowSplit split = row_split(c.k.D, sizeof(T));
     RowNormParams k = c.k;
     k.P = split.P;
     return with_row_split(split, [&](auto C, auto block) {
-        // more blocks than an SM holds at a time: a block that has stored its rows leaves room for one that loads
         const int per_block = block() ? 1 : ROWNORM_THREADS / 32 * (32 / k.P), threads = block() ? split.threads : ROWNORM_THREADS;
-        const unsigned grid = fewer((k.total + (long long)per_block - 1) / per_block, 148LL * 64);
-        if (c.vec) row_norm_kernel<T, C(), block(), true, MODE><<<grid, threads, 0, st>>>(k);
-        else row_norm_kernel<T, C(), block(), false, MODE><<<grid, threads, 0, st>>>(k);
-        g_launches += 1;
-        return cuda_status(cudaGetLastError());
+        const auto run = [&](auto vec) {
+            constexpr auto kern = row_norm_kernel<T, decltype(C)::value, decltype(block)::value, decltype(vec)::value, MODE>;
+            const long long most = resident_blocks<kern>(*dev, threads);
+            if (most == 0) return (int)TVM_ATTN_CUDA_ERROR;
+            kern<<<fewer((k.total + (long long)per_block - 1) / per_block, most), threads, 0, st>>>(k);
+            g_launches += 1;
+            return cuda_status(cudaGetLastError());
+        };
+        return c.vec ? run(std::true_type()) : run(std::false_type());
     });
 }
 
