@@ -259,7 +259,7 @@ int tvm_attn_quantize_s8(const tvm_attn_rows_params* p, const tvm_attn_rows* x, 
  * The sum is exact; the scaling is fp32, rounded once to the output's type.
  *   in : q (M, K), w (N, K) signed 8-bit integers (-128 too); s: M floats, ws: N floats; bias: N floats or NULL
  *   out: y (M, N) of `dtype`
- * K <= 65536 (TVM_ATTN_UNSUPPORTED beyond).  Rows of q and w begin on 16 bytes: pointers 16-byte aligned, ldq and ldw multiples
+ * K <= 65536, M and N <= 2^30 (TVM_ATTN_UNSUPPORTED beyond).  Rows of q and w begin on 16 bytes: pointers 16-byte aligned, ldq and ldw multiples
  * of 16 and >= K (what lies between K and ldq is not read).  y is aligned to its element, ldy >= N.  M = 0 is a call without rows.
  */
 typedef struct {

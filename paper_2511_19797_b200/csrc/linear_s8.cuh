@@ -9,9 +9,10 @@
 // the tensor cores.  Warp 0 loads by TMA, warp 1 of the pair's first CTA issues the MMAs, warps 4 to 11 scale and store one
 // accumulator while the other one fills; a pair walks over its tiles, and the ring of loads runs on through them.
 //
-// Few rows: the weights' bytes are all there is.  mma.sync with 16 channels and 8 rows a warp: operands go from global memory
-// straight to registers (a contraction does not care about the order of k: a lane's 16 contiguous bytes serve as its four
-// operand words), the warps of a block share k, and the partial sums, integers, are added in shared memory.
+// Up to 256 rows the weights' bytes are what a product costs, and they stream past the tokens: the weights are then the tensor cores'
+// operand with 128 rows, and the CTAs of a cluster share k.  Up to 2 rows (single tokens) dp4a on operands that go from global memory
+// straight to registers keeps pace with HBM: nothing is set up, and nothing waits.  (mma.sync, which emulates 8-bit products on this
+// GPU at some 150 multiply-adds a cycle and SM, took 20 us for one token and 14336 x 4096 weights.)
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -30,7 +31,7 @@ struct LinearParams {
     void* y;
     long long ldq, ldw, ldy;   // elements between rows
     int M, N, K;
-    int ksplit;          // few rows: warps of a block that share k (1, 2, 4, 8)
+    int ksplit;                // some rows: CTAs of a cluster, which share k
     int tiles_m, tiles_n;      // many rows
     int tma_out;               // whether y's rows begin on 16 bytes
     int* status;               // device status word; non-zero makes the kernel a no-op
@@ -41,7 +42,7 @@ template <> __device__ __forceinline__ float linear_round<float>(float v) { retu
 template <> __device__ __forceinline__ __nv_bfloat16 linear_round<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
 // ------------------------------------------------------------------------------------------------ few rows
-constexpr int LIN_FEW_THREADS = 256, LIN_FEW_UNROLL = 4;
+constexpr int LIN_FEW_THREADS = 128, LIN_FEW_LOADS = 8;   // 16-byte loads of weights that a lane has in flight
 
 // 16 bytes of a row of k, zeros behind its end (the memory behind it is not read).
 __device__ __forceinline__ uint4 linear_load16(const int8_t* row, int k, int K, bool stream) {
@@ -59,64 +60,52 @@ __device__ __forceinline__ uint4 linear_load16(const int8_t* row, int k, int K, 
     return v;
 }
 
-__device__ __forceinline__ void linear_mma16832(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-// NT groups of 8 rows of q a block.
-template <typename OUT, int NT>
+// Up to MT tokens, R channels a warp; the lanes share k.  All warps are resident at once: what an SM has more of than others costs
+// nothing, since HBM is the bound and not the SM.
+template <typename OUT, int MT, int R>
 __global__ void __launch_bounds__(LIN_FEW_THREADS) linear_s8_few_kernel(const LinearParams p) {
-    constexpr int WARPS = LIN_FEW_THREADS / 32, PITCH = 20;   // (16 channels of a token, and 4 against bank conflicts)
-    __shared__ int part[WARPS][8 * NT][PITCH];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int KS = p.ksplit, RW = WARPS / KS, ks = warp % KS, rg = warp / KS;
-    const int n0 = (blockIdx.x * RW + rg) * 16;
-    const long long m0 = (long long)blockIdx.y * (8 * NT);
-    int acc[NT][4];
+    constexpr int U = LIN_FEW_LOADS / R;
+    const int lane = threadIdx.x & 31, n0 = (blockIdx.x * (LIN_FEW_THREADS / 32) + (threadIdx.x >> 5)) * R;
+    if (n0 >= p.N) return;
+    int acc[R][MT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0;
-    const bool lo_ok = n0 + g < p.N, hi_ok = n0 + g + 8 < p.N;
-    const int8_t* w_lo = p.w + (lo_ok ? (long long)(n0 + g) * p.ldw : 0);
-    const int8_t* w_hi = p.w + (hi_ok ? (long long)(n0 + g + 8) * p.ldw : 0);
-    for (int k0 = ks * 64 * LIN_FEW_UNROLL; k0 < p.K; k0 += KS * 64 * LIN_FEW_UNROLL) {
-        uint4 lo[LIN_FEW_UNROLL], hi[LIN_FEW_UNROLL];
+    for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int u = 0; u < LIN_FEW_UNROLL; ++u) {
-            const int k = k0 + 64 * u + 16 * t;
-            lo[u] = linear_load16(w_lo, lo_ok ? k : p.K, p.K, true);
-            hi[u] = linear_load16(w_hi, hi_ok ? k : p.K, p.K, true);
-        }
+        for (int m = 0; m < MT; ++m) acc[r][m] = 0;
+    const int8_t* w[R];
 #pragma unroll
-        for (int u = 0; u < LIN_FEW_UNROLL; ++u) {
-            const int k = k0 + 64 * u + 16 * t;
+    for (int r = 0; r < R; ++r) w[r] = p.w + (long long)(n0 + r < p.N ? n0 + r : n0) * p.ldw;
+    for (int k0 = 16 * lane; k0 < p.K; k0 += 512 * U) {
+        uint4 b[U][R];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const long long m = m0 + 8 * j + g;
-                const uint4 x = linear_load16(p.q + (m < p.M ? m : 0) * p.ldq, m < p.M ? k : p.K, p.K, false);
-                linear_mma16832(acc[j], lo[u].x, hi[u].x, lo[u].y, hi[u].y, x.x, x.y);
-                linear_mma16832(acc[j], lo[u].z, hi[u].z, lo[u].w, hi[u].w, x.z, x.w);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < R; ++r) b[u][r] = linear_load16(w[r], k0 + 512 * u, p.K, true);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const uint4 x = linear_load16(p.q + (m < p.M ? m * p.ldq : 0), m < p.M ? k0 + 512 * u : p.K, p.K, false);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    acc[r][m] = __dp4a((int)b[u][r].x, (int)x.x, acc[r][m]);
+                    acc[r][m] = __dp4a((int)b[u][r].y, (int)x.y, acc[r][m]);
+                    acc[r][m] = __dp4a((int)b[u][r].z, (int)x.z, acc[r][m]);
+                    acc[r][m] = __dp4a((int)b[u][r].w, (int)x.w, acc[r][m]);
+                }
             }
-        }
     }
+    int mine = 0;   // of token lane / R and channel lane % R
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        part[warp][8 * j + 2 * t][g] = acc[j][0];
-        part[warp][8 * j + 2 * t + 1][g] = acc[j][1];
-        part[warp][8 * j + 2 * t][g + 8] = acc[j][2];
-        part[warp][8 * j + 2 * t + 1][g + 8] = acc[j][3];
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < RW * 16 * 8 * NT; i += LIN_FEW_THREADS) {
-        const int c = i % (RW * 16), j = i / (RW * 16), n = blockIdx.x * RW * 16 + c;
-        const long long m = m0 + j;
-        if (n >= p.N || m >= p.M) continue;
-        int sum = 0;
-        for (int k = 0; k < KS; ++k) sum += part[(c / 16) * KS + k][j][c % 16];
-        const float v = (float)sum * p.s[m] * p.ws[n];
-        static_cast<OUT*>(p.y)[m * p.ldy + n] = linear_round<OUT>(p.bias ? v + p.bias[n] : v);
-    }
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int sum = __reduce_add_sync(0xffffffffu, acc[r][m]);
+            if (lane == m * R + r) mine = sum;
+        }
+    const int m = lane / R, n = n0 + lane % R;
+    if (m < MT && m < p.M && n < p.N)
+        static_cast<OUT*>(p.y)[m * p.ldy + n] = linear_round<OUT>(fmaf((float)mine * p.s[m], p.ws[n], p.bias ? p.bias[n] : 0.f));
 }
 
 // ------------------------------------------------------------------------------------------------ many rows
@@ -385,6 +374,153 @@ linear_s8_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__
     ptx::cluster_sync();   // neither CTA leaves, or frees its tensor memory, while the other one may still reach into it
     ptx::tc_fence_after_sync();
     if (warp == 2) ptx::tmem_dealloc_pair(tmem, C::TMEM_COLS);
+    if (threadIdx.x == 0 && flags[0]) atomicExch(p.status, 1);
+}
+
+// ------------------------------------------------------------------------------------------------ some rows
+// Up to 256 rows: the weights stream past the tokens, so they are the operand with 128 rows (channels), the tokens the one with NT columns,
+// and the cluster's CTAs share k.  When all are done, each writes its partial sums, integers, of a token into the shared memory of the
+// CTA that adds them up (writes do not wait for one another; fetched by reads, 64 tokens took 4 us more).  Up to 64 tokens three
+// CTAs an SM: what it has in flight is 150 KB and more.
+constexpr int LIN_THIN_THREADS = 192;
+
+template <int NT>
+struct ThinCfg {
+    static constexpr int W_BYTES = 128 * 128, Q_BYTES = NT * 128, STAGE = W_BYTES + Q_BYTES;
+    static constexpr int STAGES = NT <= 16 ? 4 : NT <= 128 ? 3 : 4, RESIDENT = NT <= 64 ? 3 : NT <= 128 ? 2 : 1;
+    static constexpr int O_BARRIERS = STAGES * STAGE, SMEM_BYTES = O_BARRIERS + 128 + 1024;
+    static constexpr uint32_t TMEM_COLS = NT < 32 ? 32 : NT;
+    // (NT / 4 + 7) / parts groups of four tokens and 128 channels from each of up to 8 CTAs
+    static_assert((NT / 4 + 7) * 2048 <= STAGES * STAGE && (2 * STAGES + 2) * 8 + 16 <= 128 && RESIDENT * (SMEM_BYTES + 1024) <= 228 * 1024, "");
+};
+
+template <int NT, typename OUT>
+__global__ void __launch_bounds__(LIN_THIN_THREADS)
+linear_s8_thin_kernel(const __grid_constant__ CUtensorMap mw, const __grid_constant__ CUtensorMap mq, const LinearParams p) {
+    using C = ThinCfg<NT>;
+    extern __shared__ uint8_t smem[];
+    const uint32_t base = (ptx::smem_u32(smem) + 1023u) & ~1023u, bars = base + C::O_BARRIERS;
+    auto full = [&](int s) { return bars + 8 * s; };
+    auto empty = [&](int s) { return bars + 8 * (C::STAGES + s); };
+    const uint32_t done = bars + 8 * (2 * C::STAGES), drain = done + 8, flag_addr = done + 16;
+    volatile int* flags = static_cast<volatile int*>(__cvta_shared_to_generic(flag_addr));   // abort, skip, tensor-memory address
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, parts = p.ksplit;
+    const int part = parts > 1 ? (int)ptx::cluster_rank() : 0, tile = blockIdx.x / parts;
+    const int kblocks = (p.K + 127) / 128, first = (int)((long long)kblocks * part / parts), last = (int)((long long)kblocks * (part + 1) / parts);
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) { ptx::mbar_init(full(s), 1); ptx::mbar_init(empty(s), 1); }
+        ptx::mbar_init(done, 1);
+        ptx::mbar_init(drain, 1);
+        flags[0] = 0;
+        flags[1] = *reinterpret_cast<volatile int*>(p.status);   // an earlier kernel timed out: nothing is computed
+        ptx::fence_mbar_init();
+    }
+    if (warp == 1) { ptx::tmem_alloc(flag_addr + 8, C::TMEM_COLS); ptx::tmem_relinquish(); }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = flags[2];
+    const bool skip = flags[1];
+    if (skip) {
+    } else if (warp == 0) {
+        const uint32_t el = ptx::elect_one();
+        int s = 0;
+        uint32_t phase = 1;
+        bool ok = true;
+        for (int kb = first; kb < last && ok; ++kb) {
+            ok = ptx::mbar_wait_warp_s(empty(s), phase, flag_addr, LIN_WAIT_LIMIT_NS);
+            if (ok && el) {
+                ptx::mbar_arrive_expect_tx(full(s), C::STAGE);
+                ptx::tma_load_2d(base + s * C::STAGE, &mw, full(s), kb * 128, tile * 128);
+                ptx::tma_load_2d(base + s * C::STAGE + C::W_BYTES, &mq, full(s), kb * 128, 0);
+            }
+            __syncwarp();
+            if (++s == C::STAGES) { s = 0; phase ^= 1; }
+        }
+        if (!ok)   // loads in flight land within microseconds, the block leaves after two milliseconds
+            for (const uint64_t t0 = ptx::globaltimer_ns(); ptx::globaltimer_ns() - t0 < ptx::DRAIN_LIMIT_NS;) __nanosleep(1000);
+    } else if (warp == 1) {
+        constexpr uint32_t IDESC = ptx::idesc_s8_s32(128, NT), HI = ptx::desc_hi_sw128(1024);
+        const uint32_t el = ptx::elect_one();
+        int s = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int kb = first; kb < last; ++kb) {
+            ok = ptx::mbar_wait_warp_s(full(s), phase, flag_addr, LIN_WAIT_LIMIT_NS);
+            if (!ok) break;
+            ptx::tc_fence_after_sync();
+            const uint32_t a = ptx::desc_lo(base + s * C::STAGE, 16), b = ptx::desc_lo(base + s * C::STAGE + C::W_BYTES, 16);
+            const int steps = p.K - kb * 128 > 96 ? 4 : (p.K - kb * 128 + 31) / 32;   // (behind K there are zeros)
+            for (int i = 0; i < steps; ++i) ptx::mma_s8(el, tmem, a + 2 * i, b + 2 * i, HI, IDESC, kb > first || i > 0);
+            ptx::mma_commit_p(el, empty(s));
+            if (++s == C::STAGES) { s = 0; phase ^= 1; }
+        }
+        if (ok) ptx::mma_commit_p(el, done);
+        else {   // the MMAs in flight end before the tensor memory is freed
+            ptx::mma_commit_p(el, drain);
+            ptx::mbar_wait_drain(drain, 0, ptx::DRAIN_LIMIT_NS);
+        }
+    }
+    const int quad = warp & 3, channel = quad * 32 + lane, n = tile * 128 + channel;
+    bool ok = !skip && warp >= 2 && ptx::mbar_wait_warp_s(done, 0, flag_addr, LIN_WAIT_LIMIT_NS);
+    if (ok) ptx::tc_fence_after_sync();
+    const bool in = ok && n < p.N;
+    const float wsc = in ? __ldg(p.ws + n) : 0.f, bias = in && p.bias ? __ldg(p.bias + n) : 0.f;
+    auto store = [&](int m, int sum, float sm) { static_cast<OUT*>(p.y)[m * p.ldy + n] = linear_round<OUT>(fmaf((float)sum * sm, wsc, bias)); };
+    // Each CTA adds up the same number of tokens, four by four: the sums of four tokens and a channel are 16 bytes of each CTA's.
+    const int quads = ((p.M + 3) / 4 + parts - 1) / parts;
+    __syncwarp();
+    if (parts > 1) ptx::cluster_sync();   // all loads have landed, all MMAs have read them: the rings' memory is free
+    if (ok) {
+        int to = 0, slot = 0;
+#pragma unroll 1
+        for (int c = 0; c < NT && c < p.M; c += 16) {
+            uint32_t r[16];
+            ptx::tmem_ld16(tmem + ((uint32_t)(quad * 32) << 16) + c, r);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                if (parts > 1) {
+                    if (to < parts) ptx::st_cluster_v4(ptx::cluster_address(base + ((part * quads + slot) * 128 + channel) * 16, to), r[j], r[j + 1], r[j + 2], r[j + 3]);
+                    if (++slot == quads) { slot = 0; ++to; }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (c + j + e < p.M && in) store(c + j + e, (int)r[j + e], __ldg(p.s + c + j + e));
+                }
+            }
+        }
+    }
+    __syncwarp();
+    ptx::tc_fence_before_sync();
+    if (parts > 1) {
+        ptx::cluster_sync();
+        const int4* sums = static_cast<const int4*>(__cvta_shared_to_generic(base)) + channel;
+        const int m0 = part * quads * 4;   // the first of this CTA's tokens
+        for (int i0 = 0; i0 < quads && m0 + 4 * i0 < p.M; i0 += 8) {
+            // the scales of the next 32 tokens, a lane each
+            const float sv = m0 + 4 * i0 + lane < p.M ? __ldg(p.s + m0 + 4 * i0 + lane) : 0.f;
+#pragma unroll 2
+            for (int i = 0; i < 8; ++i) {
+                if (i0 + i >= quads) break;
+                int4 sum = make_int4(0, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const int4 v = r < parts ? sums[(r * quads + i0 + i) * 128] : make_int4(0, 0, 0, 0);
+                    sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+                }
+                const int m = m0 + 4 * (i0 + i), all[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float sm = __shfl_sync(0xffffffffu, sv, 4 * i + e);
+                    if (in && m + e < p.M) store(m + e, all[e], sm);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    if (warp == 1) ptx::tmem_dealloc(tmem, C::TMEM_COLS);
     if (threadIdx.x == 0 && flags[0]) atomicExch(p.status, 1);
 }
 

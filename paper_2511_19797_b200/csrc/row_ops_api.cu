@@ -264,25 +264,20 @@ int tvm_attn_quantize_s8(const tvm_attn_rows_params* p, const tvm_attn_rows* x, 
 namespace tvm_attn {
 
 // ------------------------------------------------------------------------------------------------ 8-bit products
-template <typename OUT, int NT>
+template <typename OUT, int MT, int R>
 static int launch_few(const LinearParams& p, cudaStream_t st) {
-    const int rows = 16 * (LIN_FEW_THREADS / 32 / p.ksplit);
-    const dim3 grid((unsigned)((p.N + rows - 1) / rows), (unsigned)((p.M + 8 * NT - 1) / (8 * NT)));
-    linear_s8_few_kernel<OUT, NT><<<grid, LIN_FEW_THREADS, 0, st>>>(p);
+    const int rows = R * (LIN_FEW_THREADS / 32);
+    linear_s8_few_kernel<OUT, MT, R><<<(unsigned)((p.N + rows - 1) / rows), LIN_FEW_THREADS, 0, st>>>(p);
     g_launches += 1;
     return cuda_status(cudaGetLastError());
 }
 
-template <typename OUT>
-static int linear_few(LinearParams p, cudaStream_t st) {
-    // warps of a block that share k: until there are some 16 warps for every SM, or 256 bytes of k for each
-    const long long groups = (p.N + 15) / 16;
-    p.ksplit = 1;
-    while (p.ksplit < 8 && groups * p.ksplit < 148 * 16 && p.K > 64 * LIN_FEW_UNROLL * p.ksplit) p.ksplit *= 2;
-    if (p.M <= 8) return launch_few<OUT, 1>(p, st);
-    if (p.M <= 16) return launch_few<OUT, 2>(p, st);
-    if (p.M <= 32) return launch_few<OUT, 4>(p, st);
-    return launch_few<OUT, 8>(p, st);
+template <typename OUT, int MT>
+static int linear_few(const LinearParams& p, cudaStream_t st) {
+    // channels a warp: as many as leave 16 warps for each SM
+    if (p.N >= 148 * 16 * 4) return launch_few<OUT, MT, 4>(p, st);
+    if (p.N >= 148 * 16 * 2) return launch_few<OUT, MT, 2>(p, st);
+    return launch_few<OUT, MT, 1>(p, st);
 }
 
 // A matrix (rows, cols) in boxes of box_cols x box_rows; what lies outside it reads as zero and is not written.
@@ -324,34 +319,101 @@ static int launch_many(LinearParams p, const DeviceFacts& dev, cudaStream_t st) 
     return cuda_status(cudaGetLastError());
 }
 
+// Cycles of a product in tiles of 256 rows, and the width of a tile: the one whose rounds of tiles take least.  What an SM loads bounds
+// them (62 bytes a cycle from L2, 128 + BN / 2 rows of k for each of a pair's CTAs: 446 cycles per 128 bytes of k at 192 channels, 402 at
+// 128), not its MMAs.  -1: more tiles than there can be.
+static long long many_cycles(const LinearParams& p, const DeviceFacts& dev, int* width) {
+    const long long tiles_m = (p.M + 2 * LIN_ROWS - 1) / (2 * LIN_ROWS), pairs = dev.sms / 2, kblocks = (p.K + 127) / 128;
+    if (tiles_m * ((p.N + 63) / 64) > 2147483647LL) return -1;
+    long long least = -1;
+    for (int bn : {256, 192, 128, 64}) {
+        const long long rounds = (tiles_m * ((p.N + bn - 1) / bn) + pairs - 1) / pairs, cost = rounds * kblocks * (256 + bn) * 6 / 5;
+        if (least < 0 || cost < least) { least = cost; *width = bn; }
+    }
+    return least;
+}
+
+template <int NT, typename OUT>
+static int launch_thin(LinearParams p, const DeviceFacts& dev, cudaStream_t st) {
+    using C = ThinCfg<NT>;
+    constexpr auto kern = linear_s8_thin_kernel<NT, OUT>;
+    thread_local unsigned long long prepared = 0;   // once per thread and context
+    if (prepared != dev.ctx) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES) != cudaSuccess) { cudaGetLastError(); return TVM_ATTN_CUDA_ERROR; }
+        prepared = dev.ctx;
+    }
+    CUtensorMap mw, mq;
+    int rc = matrix_map(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.w, p.K, p.N, p.ldw, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc == TVM_ATTN_OK) rc = matrix_map(&mq, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.q, p.K, p.M, p.ldq, 128, NT, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc != TVM_ATTN_OK) return rc;
+    p.status = dev.status;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((p.N + 127) / 128) * p.ksplit);
+    cfg.blockDim = dim3(LIN_THIN_THREADS);
+    cfg.dynamicSmemBytes = C::SMEM_BYTES;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.ksplit;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, mw, mq, p);
+    if (e != cudaSuccess) { cudaGetLastError(); return TVM_ATTN_CUDA_ERROR; }
+    g_launches += 1;
+    return TVM_ATTN_OK;
+}
+
 template <typename OUT>
-static int linear_many(const LinearParams& p, cudaStream_t st) {
+static int linear_thin(const LinearParams& p, const DeviceFacts& dev, cudaStream_t st) {
+    if (p.M <= 16) return launch_thin<16, OUT>(p, dev, st);
+    if (p.M <= 32) return launch_thin<32, OUT>(p, dev, st);
+    if (p.M <= 64) return launch_thin<64, OUT>(p, dev, st);
+    return p.M <= 128 ? launch_thin<128, OUT>(p, dev, st) : launch_thin<256, OUT>(p, dev, st);
+}
+
+// Cycles of a product on linear_s8_thin_kernel, by its number of CTAs that share k: an SM's CTAs share its loads (62 bytes a cycle) and the
+// writes of their sums (26 cycles a token), and add up some tokens each (125 cycles a token).
+static long long thin_cycles(const LinearParams& p, const DeviceFacts& dev, int split) {
+    const int NT = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : p.M <= 128 ? 128 : 256;
+    const long long tiles = (p.N + 127) / 128, kblocks = (p.K + 127) / 128, ctas = (tiles * split + dev.sms - 1) / dev.sms;
+    return ctas * ((kblocks + split - 1) / split * (128 + NT) * 2 + (split > 1 ? 26LL * p.M : 0)) + 125LL * ((p.M + split - 1) / split);
+}
+
+template <typename OUT>
+static int linear(LinearParams p, cudaStream_t st) {
     const DeviceFacts* dev;
     const int rc = tensor_core_device(&dev);
     if (rc != TVM_ATTN_OK) return rc;
-    // the width of a tile: the one whose rounds of tiles take least.  What an SM loads bounds them (62 bytes a cycle from L2,
-    // 128 + BN / 2 rows of k for each of a pair's CTAs: 446 cycles per 128 bytes of k at 192 channels, 402 at 128), not its MMAs
-    const long long tiles_m = (p.M + 2 * LIN_ROWS - 1) / (2 * LIN_ROWS), pairs = dev->sms / 2;
-    if (tiles_m * ((p.N + 63) / 64) > 2147483647LL) return TVM_ATTN_UNSUPPORTED;
-    int best = 256;
-    long long least = -1;
-    for (int bn : {256, 192, 128, 64}) {
-        const long long rounds = (tiles_m * ((p.N + bn - 1) / bn) + pairs - 1) / pairs, cost = rounds * (256 + bn);
-        if (least < 0 || cost < least) { least = cost; best = bn; }
+    // One or two tokens on dp4a, unless the products are so long that they take longer than the weights' bytes.  14336 x 4096 weights, one
+    // token 12.3 us (16.5 on the tensor cores), two 13.6; 4096 x 14336 one 14.0 (16.5), two 17.9 (16.5).
+    if (p.M <= 2 && (long long)p.M * p.K <= 16384) return p.M == 1 ? linear_few<OUT, 1>(p, st) : linear_few<OUT, 2>(p, st);
+    int bn = 0;
+    const long long many = many_cycles(p, *dev, &bn);
+    if (p.M <= 256) {
+        // Weights past the tokens, k shared by as many CTAs as is fastest, where that beats tiles of 256 rows.  Estimates of both in
+        // thousands of cycles, times in us (thin, many): 128 tokens x (4096 x 14336) 24, 43: 23.7, 30.5; x (1152 x 4608) 8, 14: 10.3, 14.4; x (14336 x
+        // 4096) 32, 20: 23.7, 22.6; x (4608 x 1152) 11, 4: 18.7, 8.3; 16 tokens x (4608 x 1152) 2.3, 3.5: 8.3, 8.3 to 10.3.
+        const int kblocks = (p.K + 127) / 128;
+        // up to 64 tokens three CTAs of an SM together keep enough of the weights in flight: as many share k as are resident (two of them, 14336 x
+        // 4096: 18.6 instead of 16.5 us); then the number of them that is fastest
+        const long long tiles = (p.N + 127) / 128, resident = 3LL * dev->sms / tiles, most = kblocks < 8 ? kblocks : 8;
+        const int least = p.M > 64 || resident < 1 ? 1 : (int)(resident < most ? resident : most);
+        long long thin = -1;
+        for (int split = least; split <= (p.M > 64 ? most : least); ++split) {
+            const long long c = thin_cycles(p, *dev, split);
+            if (thin < 0 || c < thin) { thin = c; p.ksplit = split; }
+        }
+        if (thin <= many || many < 0) return linear_thin<OUT>(p, *dev, st);
     }
-    switch (best) {
+    switch (bn) {
         case 256: return launch_many<256, OUT>(p, *dev, st);
         case 192: return launch_many<192, OUT>(p, *dev, st);
         case 128: return launch_many<128, OUT>(p, *dev, st);
-        default: return launch_many<64, OUT>(p, *dev, st);
+        case 64: return launch_many<64, OUT>(p, *dev, st);
+        default: return TVM_ATTN_UNSUPPORTED;   // more tiles than 31 bits hold
     }
 }
-
-// Up to this many rows the weights' bytes are what a product costs.
-constexpr int LIN_FEW_ROWS = 64;
-
-template <typename OUT>
-static int linear(const LinearParams& p, cudaStream_t st) { return p.M <= LIN_FEW_ROWS ? linear_few<OUT>(p, st) : linear_many<OUT>(p, st); }
 
 }  // namespace tvm_attn
 
@@ -362,7 +424,7 @@ extern "C" int tvm_attn_linear_s8(const tvm_attn_linear_params* p, const void* q
     const long long ldq = p->ldq ? p->ldq : p->K, ldw = p->ldw ? p->ldw : p->K, ldy = p->ldy ? p->ldy : p->N;
     if (ldq < p->K || ldw < p->K || ldy < p->N || ldq % 16 || ldw % 16) return TVM_ATTN_INVALID_ARG;
     // sums of K products of at most 2^14 in 32 bits; strides as a tensor map holds them
-    if (p->K > 65536 || ldq >= (1LL << 38) || ldw >= (1LL << 38) || ldy >= (1LL << 36)) return TVM_ATTN_UNSUPPORTED;
+    if (p->K > 65536 || p->M > 1 << 30 || p->N > 1 << 30 || ldq >= (1LL << 38) || ldw >= (1LL << 38) || ldy >= (1LL << 36)) return TVM_ATTN_UNSUPPORTED;
     if (p->M == 0) return TVM_ATTN_OK;
     const int esz = p->dtype == TVM_ATTN_FP32 ? 4 : 2;
     if (!q || !s || !w || !ws || !y || !aligned16(q) || !aligned16(w) || reinterpret_cast<uintptr_t>(y) % esz) return TVM_ATTN_INVALID_ARG;

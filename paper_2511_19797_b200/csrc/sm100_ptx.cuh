@@ -339,6 +339,9 @@ __device__ __forceinline__ int ld_cluster(uint32_t addr) {
     asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
 // An arrival on a barrier of the cluster (a cluster address).  Not with .release.cluster: that waits until this thread's writes
 // are visible to the cluster, 1500 to 3000 cycles behind bulk stores, where nothing but tensor memory has to be handed over.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
@@ -350,6 +353,11 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const void* tmap,
         "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1)
         : "memory");
+}
+// The same with a barrier of this CTA.
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, uint32_t bar, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1) : "memory");
 }
 // Stores one box from shared memory; what lies outside the tensor is not written.
 __device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t src, int c0, int c1) {
@@ -379,6 +387,18 @@ __device__ __forceinline__ void mma_s8_pair(uint32_t el, uint32_t d_tmem, uint32
         "mov.b64 a, {%2, %4};\n\t"
         "mov.b64 b, {%3, %4};\n\t"
         "@e tcgen05.mma.cta_group::2.kind::i8 [%1], a, b, %5, p;\n\t}"
+        ::"r"(el), "r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// kind::i8 on one CTA.
+__device__ __forceinline__ void mma_s8(uint32_t el, uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .pred e;\n\t.reg .b64 a;\n\t.reg .b64 b;\n\t"
+        "setp.ne.b32 e, %0, 0;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "mov.b64 a, {%2, %4};\n\t"
+        "mov.b64 b, {%3, %4};\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::i8 [%1], a, b, %5, p;\n\t}"
         ::"r"(el), "r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
         : "memory");
 }
