@@ -119,7 +119,7 @@ struct LinCfg {
     static constexpr int A_BYTES = LIN_ROWS * 128, B_BYTES = BN / 2 * 128, STAGE = A_BYTES + B_BYTES;
     // The epilogue works on units of 128 bytes of 32 rows, which its eight warps, two for each 32 rows of the accumulator, take in turn.
     static constexpr int UNIT = 128 / (int)sizeof(OUT), UNITS = BN / UNIT, WARP_UNITS = (UNITS + 1) / 2, UNIT_BYTES = 32 * 128;
-    static constexpr int BUFS = 2, STAGING = 8 * BUFS * UNIT_BYTES, WARP_COLS = WARP_UNITS * UNIT, TABLES = 8 * 2 * WARP_COLS * 4;
+    static constexpr int BUFS = 1, STAGING = 8 * BUFS * UNIT_BYTES, WARP_COLS = WARP_UNITS * UNIT, TABLES = 8 * 2 * WARP_COLS * 4;
     static constexpr int BARRIERS = 256, MOST = 227 * 1024 - 1024;
     static constexpr int STAGES = (MOST - STAGING - TABLES - BARRIERS) / STAGE < 8 ? (MOST - STAGING - TABLES - BARRIERS) / STAGE : 8;
     static constexpr int O_STAGING = STAGES * STAGE, O_TABLES = O_STAGING + STAGING, O_BARRIERS = O_TABLES + TABLES;
@@ -331,7 +331,7 @@ __device__ __forceinline__ void linear_store(const LinearParams& p, const LinBlo
                 }
                 __syncwarp();
             }
-            buf ^= 1;
+            buf = C::BUFS == 2 ? buf ^ 1 : 0;
             if (last) break;
         }
     }
