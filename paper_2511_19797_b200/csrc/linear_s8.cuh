@@ -65,6 +65,8 @@ __device__ __forceinline__ uint4 linear_load16(const int8_t* row, int k, int K, 
 template <typename OUT, int MT, int R>
 __global__ void __launch_bounds__(LIN_FEW_THREADS) linear_s8_few_kernel(const LinearParams p) {
     constexpr int U = LIN_FEW_LOADS / R;
+    ptx::dependency_wait();
+    ptx::dependents_launch();
     const int lane = threadIdx.x & 31, n0 = (blockIdx.x * (LIN_FEW_THREADS / 32) + (threadIdx.x >> 5)) * R;
     if (n0 >= p.N) return;
     int acc[R][MT];
@@ -353,16 +355,17 @@ linear_s8_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__
         for (int a = 0; a < 2; ++a) { ptx::mbar_init(k.acc_full(a), 1); ptx::mbar_init(k.acc_empty(a), 2 * 8); }
         ptx::mbar_init(k.drain(), 1);
         flags[0] = 0;
-        flags[1] = *reinterpret_cast<volatile int*>(p.status);   // an earlier kernel timed out: both CTAs do nothing if either sees it
         ptx::fence_mbar_init();
     }
-    __syncwarp();
-    ptx::cluster_sync();
-    const bool skip = ptx::ld_cluster(ptx::cluster_address(k.flags() + 4, 0)) | ptx::ld_cluster(ptx::cluster_address(k.flags() + 4, 1));
     if (warp == 2) ptx::tmem_alloc_pair(k.flags() + 8, C::TMEM_COLS);
+    ptx::dependency_wait();
+    ptx::dependents_launch();
+    if (threadIdx.x == 0) flags[1] = *reinterpret_cast<volatile int*>(p.status);   // an earlier kernel timed out: both CTAs do nothing if either sees it
+    __syncwarp();
     ptx::tc_fence_before_sync();
     ptx::cluster_sync();
     ptx::tc_fence_after_sync();
+    const bool skip = ptx::ld_cluster(ptx::cluster_address(k.flags() + 4, 0)) | ptx::ld_cluster(ptx::cluster_address(k.flags() + 4, 1));
     const uint32_t tmem = flags[2];
     if (!skip) {
         if (warp == 0) linear_load<BN, OUT>(p, k, ma, mb, pair, pairs);
@@ -412,10 +415,12 @@ linear_s8_thin_kernel(const __grid_constant__ CUtensorMap mw, const __grid_const
         ptx::mbar_init(done, 1);
         ptx::mbar_init(drain, 1);
         flags[0] = 0;
-        flags[1] = *reinterpret_cast<volatile int*>(p.status);   // an earlier kernel timed out: nothing is computed
         ptx::fence_mbar_init();
     }
     if (warp == 1) { ptx::tmem_alloc(flag_addr + 8, C::TMEM_COLS); ptx::tmem_relinquish(); }
+    ptx::dependency_wait();
+    ptx::dependents_launch();
+    if (threadIdx.x == 0) flags[1] = *reinterpret_cast<volatile int*>(p.status);   // an earlier kernel timed out: nothing is computed
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();

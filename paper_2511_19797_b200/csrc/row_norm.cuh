@@ -225,6 +225,8 @@ row_norm_kernel(const RowNormParams p) {
     constexpr int V = RmsVec<T>::N, E = (int)sizeof(T);
     constexpr bool TAN = MODE == ROW_NORM_TAN;
     constexpr int N = MODE == ROW_NORM ? 1 : 2;
+    ptx::dependency_wait();
+    ptx::dependents_launch();
     __shared__ __align__(16) float slots[BLOCK ? 2 * 32 * N : 4];
     if constexpr (BLOCK) clear_slots(slots, 2 * 32 * N);
     const int lane = threadIdx.x & 31, rpw = BLOCK ? 1 : 32 / p.P;
@@ -402,6 +404,7 @@ row_norm_bwd_kernel(const RowNormParams p) {
     // Rows of four chunks a thread are read again, from L1 and L2, for the outputs: held, they and the scale would not fit into
     // registers ((1024, 16384) bf16 with tangents 202 -> 106 us).
     constexpr bool RELOAD = C > 2;
+    ptx::dependency_wait();
     __shared__ __align__(16) float slots[BLOCK ? 2 * 32 * N : 32 * V];
     if constexpr (BLOCK) clear_slots(slots, 2 * 32 * N);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rpw = BLOCK ? 1 : 32 / p.P;
@@ -543,7 +546,7 @@ row_norm_bwd_kernel(const RowNormParams p) {
     }
     if (!p.aux) return;
     // the reduction may be launched: its blocks wait for this grid's end before they read anything
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    ptx::dependents_launch();
     float* partial = p.aux + (size_t)blockIdx.x * p.D;
     if constexpr (BLOCK) {
 #pragma unroll
@@ -580,7 +583,7 @@ row_norm_bwd_kernel(const RowNormParams p) {
 __global__ void __launch_bounds__(1024) row_norm_dg_kernel(const float* __restrict__ partial, float* __restrict__ dg, int n, int D) {
     __shared__ float acc[32][8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 8 + (lane & 7);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    ptx::dependency_wait();
     float v = 0.f;
     if (j < D) {
 #pragma unroll 8

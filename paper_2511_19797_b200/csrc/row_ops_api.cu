@@ -15,6 +15,31 @@
 
 namespace tvm_attn {
 
+// Launches a kernel as a programmatic dependent of the one in front of it on the stream: its blocks are set up while that one ends, and
+// wait for its end before they touch global memory.  `cluster`: blocks of a cluster where the kernel does not say.
+template <typename... P, typename... A>
+static int launch(void (*kern)(P...), unsigned grid, int threads, int smem, cudaStream_t st, int cluster, const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 0 ? 2 : 1;
+    if (cudaLaunchKernelEx(&cfg, kern, P(args)...) != cudaSuccess) {
+        cudaGetLastError();
+        return TVM_ATTN_CUDA_ERROR;
+    }
+    g_launches += 1;
+    return TVM_ATTN_OK;
+}
+
 // ------------------------------------------------------------------------------------------------ rows
 static int check_rows_params(const tvm_attn_rows_params* p) {
     if (!p || p->B < 0 || p->T < 0 || p->D <= 0) return TVM_ATTN_INVALID_ARG;
@@ -122,9 +147,7 @@ static int launch_norm(const RowsCall& c, cudaStream_t st) {
             constexpr auto kern = row_norm_kernel<T, decltype(C)::value, decltype(block)::value, decltype(vec)::value, MODE>;
             const long long most = resident_blocks<kern>(*dev, threads);
             if (most == 0) return (int)TVM_ATTN_CUDA_ERROR;
-            kern<<<fewer((k.total + (long long)per_block - 1) / per_block, most), threads, 0, st>>>(k);
-            g_launches += 1;
-            return cuda_status(cudaGetLastError());
+            return launch(kern, fewer((k.total + (long long)per_block - 1) / per_block, most), threads, 0, st, 0, k);
         };
         return c.vec ? run(std::true_type()) : run(std::false_type());
     });
@@ -149,27 +172,12 @@ static int launch_norm_bwd(const RowsCall& c, float* dg, cudaStream_t st) {
     if (blocks > 0) {
         const int rc = with_row_split(split, [&](auto C, auto block) {
             const int threads = block() ? split.threads : ROWNORM_THREADS;
-            if (c.vec) row_norm_bwd_kernel<T, C(), block(), true, TAN><<<blocks, threads, 0, st>>>(k);
-            else row_norm_bwd_kernel<T, C(), block(), false, TAN><<<blocks, threads, 0, st>>>(k);
-            g_launches += 1;
-            return cuda_status(cudaGetLastError());
+            return c.vec ? launch(row_norm_bwd_kernel<T, C(), block(), true, TAN>, blocks, threads, 0, st, 0, k)
+                         : launch(row_norm_bwd_kernel<T, C(), block(), false, TAN>, blocks, threads, 0, st, 0, k);
         });
         if (rc != TVM_ATTN_OK) return rc;
     }
-    if (!dg) return TVM_ATTN_OK;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(k.D + 7) / 8);
-    cfg.blockDim = dim3(1024);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = blocks > 0 ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, row_norm_dg_kernel, (const float*)k.aux, dg, blocks, k.D);
-    if (e == cudaSuccess) g_launches += 1;
-    else cudaGetLastError();
-    return cuda_status(e);
+    return dg ? launch(row_norm_dg_kernel, (unsigned)(k.D + 7) / 8, 1024, 0, st, 0, k.aux, dg, blocks, k.D) : TVM_ATTN_OK;
 }
 
 static size_t norm_bwd_workspace(const tvm_attn_rows_params& p) {
@@ -267,9 +275,7 @@ namespace tvm_attn {
 template <typename OUT, int MT, int R>
 static int launch_few(const LinearParams& p, cudaStream_t st) {
     const int rows = R * (LIN_FEW_THREADS / 32);
-    linear_s8_few_kernel<OUT, MT, R><<<(unsigned)((p.N + rows - 1) / rows), LIN_FEW_THREADS, 0, st>>>(p);
-    g_launches += 1;
-    return cuda_status(cudaGetLastError());
+    return launch(linear_s8_few_kernel<OUT, MT, R>, (unsigned)((p.N + rows - 1) / rows), LIN_FEW_THREADS, 0, st, 0, p);
 }
 
 template <typename OUT, int MT>
@@ -314,9 +320,7 @@ static int launch_many(LinearParams p, const DeviceFacts& dev, cudaStream_t st) 
     p.tiles_n = (p.N + BN - 1) / BN;
     p.status = dev.status;
     const long long tiles = (long long)p.tiles_m * p.tiles_n;
-    kern<<<2 * fewer(tiles, dev.sms / 2), LIN_THREADS, C::SMEM_BYTES, st>>>(ma, mb, my, p);
-    g_launches += 1;
-    return cuda_status(cudaGetLastError());
+    return launch(kern, 2 * fewer(tiles, dev.sms / 2), LIN_THREADS, C::SMEM_BYTES, st, 0, ma, mb, my, p);
 }
 
 // Cycles of a product in tiles of 256 rows, and the width of a tile: the one whose rounds of tiles take least.  What an SM loads bounds
@@ -347,21 +351,7 @@ static int launch_thin(LinearParams p, const DeviceFacts& dev, cudaStream_t st) 
     if (rc == TVM_ATTN_OK) rc = matrix_map(&mq, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.q, p.K, p.M, p.ldq, 128, NT, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc != TVM_ATTN_OK) return rc;
     p.status = dev.status;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((p.N + 127) / 128) * p.ksplit);
-    cfg.blockDim = dim3(LIN_THIN_THREADS);
-    cfg.dynamicSmemBytes = C::SMEM_BYTES;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.ksplit;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, mw, mq, p);
-    if (e != cudaSuccess) { cudaGetLastError(); return TVM_ATTN_CUDA_ERROR; }
-    g_launches += 1;
-    return TVM_ATTN_OK;
+    return launch(kern, (unsigned)((p.N + 127) / 128) * p.ksplit, LIN_THIN_THREADS, C::SMEM_BYTES, st, p.ksplit, mw, mq, p);
 }
 
 template <typename OUT>

@@ -411,6 +411,13 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t el, uint32_t bar) {
         ::"r"(el), "r"(bar), "h"((uint16_t)3) : "memory");
 }
 
+// ---------------------------------------------------------------- dependent launches
+// Waits until the kernel in front on the stream has ended and its writes can be seen (a kernel launched in the ordinary way has nothing
+// to wait for); before it a kernel launched as a programmatic dependent touches nothing in global memory.
+__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Lets the next kernel's blocks be launched, to wait in their turn.
+__device__ __forceinline__ void dependents_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ---------------------------------------------------------------- small math helpers
 __device__ __forceinline__ float ex2(float x) {
     float y;
