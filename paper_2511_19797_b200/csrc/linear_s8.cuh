@@ -33,7 +33,7 @@ struct LinearParams {
     int M, N, K;
     int ksplit;                // some rows: CTAs of a cluster, which share k
     int tiles_m, tiles_n;      // many rows
-    int tma_out;               // whether y's rows begin on 16 bytes
+    int tma_cols;              // columns of y that bulk stores may reach into: they write 16 bytes at a time, behind the end of a row too
     int* status;               // device status word; non-zero makes the kernel a no-op
 };
 
@@ -306,14 +306,14 @@ __device__ __forceinline__ void linear_store(const LinearParams& p, const LinBlo
                 ptx::st_shared_v4(to + lane * 128 + ((i ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
             }
             const int col0 = tn * BN + u * C::UNIT;
-            if (p.tma_out) {
+            if (col0 + C::UNIT <= p.tma_cols) {
                 ptx::fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
                     if (row0 < p.M && col0 < p.N) ptx::tma_store_2d(&my, to, col0, (int)row0);
                     ptx::bulk_commit();
                 }
-            } else {   // rows that do not begin on 16 bytes: a warp stores one row after the other
+            } else {   // rows that do not begin or end on 16 bytes: a warp stores one row after the other
                 __syncwarp();
                 for (int i = 0; i < 32 && row0 + i < p.M; ++i) {
                     OUT* dst = static_cast<OUT*>(p.y) + (row0 + i) * p.ldy + col0;

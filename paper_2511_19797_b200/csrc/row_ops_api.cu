@@ -311,8 +311,9 @@ static int launch_many(LinearParams p, const DeviceFacts& dev, cudaStream_t st) 
     int rc = matrix_map(&ma, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.q, p.K, p.M, p.ldq, 128, LIN_ROWS, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == TVM_ATTN_OK) rc = matrix_map(&mb, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.w, p.K, p.N, p.ldw, 128, BN / 2, CU_TENSOR_MAP_SWIZZLE_128B);
     my = ma;   // (not used where y's rows do not begin on 16 bytes)
-    p.tma_out = aligned16(p.y) && p.ldy * (long long)sizeof(OUT) % 16 == 0;
-    if (rc == TVM_ATTN_OK && p.tma_out)
+    const bool begin = aligned16(p.y) && p.ldy * (long long)sizeof(OUT) % 16 == 0, end = p.N * (long long)sizeof(OUT) % 16 == 0;
+    p.tma_cols = !begin ? 0 : end ? INT32_MAX : p.N;
+    if (rc == TVM_ATTN_OK && begin)
         rc = matrix_map(&my, HALF ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, (int)sizeof(OUT), p.y, p.N, p.M, p.ldy, C::UNIT, 32,
                         CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc != TVM_ATTN_OK) return rc;

@@ -337,6 +337,69 @@ def test_products_into_given_rows(M, dtype):
         assert (buf == 7.0).all()                                  # nothing was written around them
 
 
+def _linear_on_gpu(q, s, w, ws, bias):
+    """The definition in 64 bits (whole numbers below 2^53 are exact in a 64-bit product of matrices), and the size of its terms."""
+    y = (q.double() @ w.double().t()) * s.double()[:, None] * ws.double()
+    b = torch.zeros_like(ws) if bias is None else bias
+    return (y + b.double()).cpu().numpy(), (y.abs() + b.double().abs()).cpu().numpy()
+
+
+# every number of CTAs that share k, tiles of 16 to 256 tokens, every width of a tile of channels, several tiles a pair
+@pytest.mark.parametrize("M,N,K", [(3, 14336, 4096), (16, 2000, 1024), (17, 9000, 896), (31, 130, 385), (40, 1152, 4608), (63, 7000, 520), (65, 768, 2304), (100, 640, 8192), (128, 128, 128),
+                                   (130, 333, 5000), (200, 1280, 6144), (255, 96, 4100), (256, 4608, 1152), (300, 4224, 768), (1000, 8200, 136), (5000, 3456, 1152), (9472, 2056, 300), (20000, 200, 64)])
+def test_products_of_every_kind(M, N, K):
+    for dtype in DTYPES:
+        (_, q), (_, w) = _rows8(M, M, K), _rows8(N, N, K)
+        s, ws, b = (_draw(K + 3, M).abs() * 1e-2).cuda(), (_draw(K + 4, N).abs() * 1e-2).cuda(), _draw(K + 5, N).cuda()
+        _close(binding.tvm_attn_linear_s8(q, s, w, ws, b, dtype=dtype), _linear_on_gpu(q, s, w, ws, b), roundings=4)
+    binding.tvm_attn_check_status()
+
+
+def test_products_of_drawn_sizes():
+    rng = np.random.default_rng(11)
+    for i in range(60):
+        M, N, K = (int(round(np.exp(rng.uniform(np.log(lo), np.log(hi))))) for lo, hi in ((1, 3000), (1, 5000), (1, 6000)))
+        dtype, bias = DTYPES[i % 2], bool(rng.integers(2))
+        (_, q), (_, w) = _rows8(i, M, K), _rows8(i + 100, N, K)
+        s, ws, b = (_draw(i, M).abs() * 1e-2).cuda(), (_draw(i + 1, N).abs() * 1e-2).cuda(), _draw(i + 2, N).cuda() if bias else None
+        got, (value, size) = binding.tvm_attn_linear_s8(q, s, w, ws, b, dtype=dtype), _linear_on_gpu(q, s, w, ws, b)
+        _close(got, (value, size), roundings=4, what=(M, N, K, dtype, bias))
+
+
+@pytest.mark.parametrize("M", [2, 70, 300])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N", [1, 7, 61, 101, 250])
+def test_products_into_rows_on_16_bytes_with_a_ragged_end(M, dtype, N):
+    """Rows of any length whose starts lie on 16 bytes: what lies behind them is left as it was."""
+    buf = torch.full((M + 2, 512), 7.0, dtype=dtype, device="cuda")
+    out = buf[1 : M + 1, 8 : 8 + N]
+    _linear_case(M, N, 200, dtype, True, out=out)
+    out.fill_(7.0)
+    assert (buf == 7.0).all()
+
+
+@pytest.mark.parametrize("M", [2, 33, 300])
+def test_product_outputs_far_apart(M):
+    N, K = 40, 64
+    gap = ((1 << 32) // (M - 1) + 64) // 16 * 16       # the last row lies beyond 2^32 elements
+    buf = torch.empty(gap * (M - 1) + 64, dtype=torch.bfloat16, device="cuda")
+    _linear_case(M, N, K, torch.bfloat16, True, out=buf.as_strided((M, N), (gap, 1), 0))
+
+
+def test_products_do_nothing_after_a_time_out_until_it_is_reported():
+    (_, q), (_, w) = _rows8(1, 300, 64), _rows8(2, 40, 64)
+    s, ws = torch.ones(300, device="cuda"), torch.ones(40, device="cuda")
+    want = binding.tvm_attn_linear_s8(q, s, w, ws)
+    for M in (300, 20):
+        y = torch.full((M, 40), 7.0, dtype=torch.bfloat16, device="cuda")
+        binding.tvm_attn_selftest_timeout(1_000_000)
+        binding.tvm_attn_linear_s8(q[:M], s[:M], w, ws, out=y)
+        with pytest.raises(binding.TvmAttnError, match="DEVICE_TIMEOUT"):
+            binding.tvm_attn_check_status()
+        assert (y == 7.0).all()
+        assert torch.equal(binding.tvm_attn_linear_s8(q[:M], s[:M], w, ws), want[:M])
+
+
 def test_product_shapes_and_strides():
     q, s = binding.tvm_attn_quantize_s8(_draw(1, 2, 3, 5, 48).cuda())
     w, ws = binding.tvm_attn_quantize_s8(_draw(2, 40, 48).cuda())
@@ -452,6 +515,28 @@ def test_captured_calls_replay_bit_for_bit():
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert torch.equal(a, b)
+
+
+def test_calls_in_a_row_wait_for_one_another():
+    """Kernels are set up while the one in front of them ends: the same buffers written and read by call after call."""
+    w, ws = binding.tvm_attn_quantize_s8(_draw(90, 640, 1152).cuda())
+    for rows in (5, 100, 3000):
+        xs = [_draw(91 + k, rows, 1152, dtype=torch.bfloat16).cuda() for k in range(4)]
+        want = []
+        for x in xs:
+            q, s, h = binding.tvm_attn_rmsnorm_s8(x, xs[0])
+            torch.cuda.synchronize()
+            want.append((h, binding.tvm_attn_linear_s8(q, s, w, ws)))
+            torch.cuda.synchronize()
+        q, s, h = binding.tvm_attn_rmsnorm_s8(xs[0], xs[0])
+        y = torch.empty(rows, 640, dtype=torch.bfloat16, device="cuda")
+        got = []
+        for i in range(24):
+            binding.tvm_attn_rmsnorm_s8(xs[i % 4], xs[0], out=(q, s, h))
+            binding.tvm_attn_linear_s8(q, s, w, ws, out=y)
+            got.append((h.clone(), y.clone()))
+        for i, (a, b) in enumerate(got):
+            assert torch.equal(a, want[i % 4][0]) and torch.equal(b, want[i % 4][1]), (rows, i)
 
 
 def test_calls_on_other_streams():
