@@ -36,8 +36,9 @@ struct RowNormParams {
 };
 
 constexpr int ROWNORM_THREADS = 256;   // of a block whose rows are on warps
+constexpr int ROWNORM_SINGLE = 160;    // chunks of a row with one on each thread, at most
 // Threads that a block with one row can have, C chunks each.
-template <typename T, int C> constexpr int rownorm_block_threads() { return C == 4 && sizeof(T) == 4 ? 1024 : C == 1 ? 160 : 512; }
+template <typename T, int C> constexpr int rownorm_block_threads() { return C == 4 && sizeof(T) == 4 ? 1024 : C == 1 ? ROWNORM_SINGLE : 512; }
 // Blocks of the backward on an SM: as many as the registers let in (a block walks over its rows from the start to the end of the
 // launch, so one that waits for another's end would double the time).  `threads`: of a block with one row, 0 for rows on warps.
 __host__ __device__ constexpr int rownorm_bwd_resident(int threads, bool tan) {
@@ -328,12 +329,12 @@ row_norm_kernel(const RowNormParams p) {
         const float root = rsqrtf(sums[0] * inv_d + p.eps * pre * pre);   // 1 / (r pre)
         const float inv = root * pre;
         if constexpr (MODE == ROW_S8) {
-            // scaled up first where 127 / max would leave the range; zeros where the maximum is not finite
-            const float top = sums[N - 1], up = top < 0x1p-100f ? 0x1p100f : 1.f;
+            // scaled first where 127 / max would leave the range of the fast division; zeros where the maximum is not finite
+            const float top = sums[N - 1], up = top < 0x1p-100f ? 0x1p100f : top > 0x1p100f ? 0x1p-100f : 1.f;
             const bool fine = top <= 3.4028235e38f && top > 0.f;
-            const float k = fine ? 127.f / (top * up) : 0.f;
+            const float k = fine ? __fdividef(127.f, top * up) : 0.f;
             if (act) {
-                if (L.c == 0) p.aux[row] = top * (p.norm ? inv : 1.f) / 127.f;
+                if (L.c == 0) p.aux[row] = top * (p.norm ? inv : 1.f) * (1.f / 127.f);
                 int8_t* to = reinterpret_cast<int8_t*>(Lane::at(y0, p.out[0], at, p));
                 const uint64_t up2 = ptx::pack2(up, up), k2 = ptx::pack2(k, k), round2 = ptx::pack2(12582912.f, 12582912.f);   // 1.5 2^23
 #pragma unroll
