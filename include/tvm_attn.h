@@ -40,8 +40,9 @@ extern "C" {
 typedef enum {
     TVM_ATTN_OK = 0,
     TVM_ATTN_INVALID_ARG = -1,         /* null pointer, non-positive dim, misaligned pointer, bad dtype/flags */
-    TVM_ATTN_UNSUPPORTED = -2,         /* d > 128 or d % 8 != 0, device is not sm_100, too many tiles  */
-    TVM_ATTN_WORKSPACE_TOO_SMALL = -3, /* workspace_bytes < tvm_attn_jvp_workspace_bytes(...) */
+    TVM_ATTN_UNSUPPORTED = -2,         /* d > 128 or d % 8 != 0, D, K or another size beyond an operator's limit, device is not
+                                          sm_100, too many tiles  */
+    TVM_ATTN_WORKSPACE_TOO_SMALL = -3, /* workspace_bytes < what the operator's ..._workspace_bytes(...) says */
     TVM_ATTN_CUDA_ERROR = -4,          /* a CUDA runtime/driver call or a launch failed */
     TVM_ATTN_DEVICE_TIMEOUT = -5,      /* a bounded on-device wait ran out (see tvm_attn_check_status) */
     TVM_ATTN_TOO_LARGE = -6            /* B*H*N exceeds the built-in scratch of tvm_attn_jvp_bwd_noalloc */
@@ -212,7 +213,7 @@ typedef struct {
 
 /*
  * RMSNorm of a sum, with a tangent (paper Sec. 4 "semi-Lipschitz control": RMSNorm in place of LayerNorm; App. "Lipschitzness of
- * RMSNorm" for the Jacobian J v = (v - u (u . v) / D) / r):
+ * RMSNorm" for the Jacobian J v = (v - u (u . v) / D) / r), rows of zeros with eps = 0 giving NaN:
  *     h = x + res    r = sqrt(mean(h^2) + eps)    u = h / r    y = g * u
  *     th = tx + tres                              ty = g * (J th)
  * The norm is that of the unrounded sum.  The sums over a row are fp32; rows whose squares leave its range are scaled first.

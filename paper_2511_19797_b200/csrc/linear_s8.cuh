@@ -65,9 +65,9 @@ __device__ __forceinline__ uint4 linear_load16(const int8_t* row, int k, int K, 
 template <typename OUT, int MT, int R>
 __global__ void __launch_bounds__(LIN_FEW_THREADS) linear_s8_few_kernel(const LinearParams p) {
     constexpr int U = LIN_FEW_LOADS / R;
+    const int lane = threadIdx.x & 31, n0 = (blockIdx.x * (LIN_FEW_THREADS / 32) + (threadIdx.x >> 5)) * R;
     ptx::dependency_wait();
     ptx::dependents_launch();
-    const int lane = threadIdx.x & 31, n0 = (blockIdx.x * (LIN_FEW_THREADS / 32) + (threadIdx.x >> 5)) * R;
     if (n0 >= p.N) return;
     int acc[R][MT];
 #pragma unroll

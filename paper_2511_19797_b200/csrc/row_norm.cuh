@@ -115,7 +115,7 @@ template <int N, typename LANE>
 __device__ __forceinline__ void row_prefetch(const RowNormParams& p, unsigned row, int bytes) {   // a thread for each tensor
     if (threadIdx.x < N && row < p.total) {
         const RowsPtr& t = p.in[threadIdx.x];
-        if (t.p) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(LANE::at(t.p, t, row, p)), "r"(bytes) : "memory");
+        if (t.p) ptx::prefetch_l2(LANE::at(t.p, t, row, p), (uint32_t)bytes);
     }
 }
 

@@ -411,6 +411,11 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t el, uint32_t bar) {
         ::"r"(el), "r"(bar), "h"((uint16_t)3) : "memory");
 }
 
+// Asks for `bytes` (a multiple of 16, from a 16-byte aligned address) to be brought into L2, which all SMs share: a hint, fulfilled or not.
+__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
+
 // ---------------------------------------------------------------- dependent launches
 // Waits until the kernel in front on the stream has ended and its writes can be seen (a kernel launched in the ordinary way has nothing
 // to wait for); before it a kernel launched as a programmatic dependent touches nothing in global memory.

@@ -704,9 +704,9 @@ uint64_t tvm_attn_launch_count(void) { return g_launches.load(); }
 const char* tvm_attn_strerror(int code) {
     switch (code) {
         case TVM_ATTN_OK: return "ok";
-        case TVM_ATTN_INVALID_ARG: return "invalid argument (null or misaligned pointer, bad dimension, dtype, flags or scale)";
-        case TVM_ATTN_UNSUPPORTED: return "unsupported shape or device (need 8 <= d <= 128, d % 8 == 0, an sm_100 GPU)";
-        case TVM_ATTN_WORKSPACE_TOO_SMALL: return "workspace smaller than tvm_attn_jvp_workspace_bytes()";
+        case TVM_ATTN_INVALID_ARG: return "invalid argument (null or misaligned pointer, bad dimension, stride, dtype, flags, scale or eps, or outputs that do not match the inputs)";
+        case TVM_ATTN_UNSUPPORTED: return "unsupported shape or device (attention: 8 <= d <= 128, d % 8 == 0; rows: D <= 16384; 8-bit products: K <= 65536; an sm_100 GPU)";
+        case TVM_ATTN_WORKSPACE_TOO_SMALL: return "workspace smaller than the entry point's ..._workspace_bytes()";
         case TVM_ATTN_CUDA_ERROR: return "a CUDA call or kernel launch failed";
         case TVM_ATTN_DEVICE_TIMEOUT: return "a bounded wait inside a kernel ran out; outputs are unspecified";
         case TVM_ATTN_TOO_LARGE: return "B*H*N exceeds TVM_ATTN_NOALLOC_MAX_ROWS, the built-in scratch of tvm_attn_jvp_bwd_noalloc; "
@@ -715,6 +715,6 @@ const char* tvm_attn_strerror(int code) {
     }
 }
 
-int tvm_attn_version(void) { return 100; }
+int tvm_attn_version(void) { return 200; }
 
 }  // extern "C"
