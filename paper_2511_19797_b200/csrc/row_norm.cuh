@@ -32,6 +32,7 @@ struct RowNormParams {
     int D, P;         // P: lanes of a row (all threads of the block where a row has one of its own)
     float eps;
     bool flat;        // every tensor is one dimension of rows less than 4 GB apart
+    bool same;        // and all have the same stride and less than 4 GB
     bool norm;        // 8-bit rows: of the norm's output (else of x + res itself)
 };
 
@@ -47,6 +48,13 @@ __host__ __device__ constexpr int rownorm_bwd_resident(int threads, bool tan) {
 // All of them.  A fixed number: the partial sums of the scale's gradient, a row per block, have a size and an order that do not
 // depend on the device.
 __host__ __device__ constexpr int rownorm_bwd_blocks(int threads, bool tan) { return 148 * rownorm_bwd_resident(threads, tan); }
+
+// `base` moved on by `row` rows of tensor t: one instruction where the rows are one dimension.
+__device__ __forceinline__ char* row_of(char* base, const RowsPtr& t, unsigned row, const RowNormParams& p) {
+    if (p.flat) return base + (size_t)row * (unsigned)t.row;
+    const unsigned b = row / p.T;
+    return base + (size_t)b * (size_t)t.batch + (size_t)(row - b * p.T) * (size_t)t.row;
+}
 
 // The lanes of one row and their columns.  VEC: a chunk is 16 contiguous bytes.  Otherwise (a pointer, stride or width that is
 // no multiple of 16 bytes) the elements of a chunk are P apart, so that an instruction still touches contiguous bytes.
@@ -97,13 +105,12 @@ struct RowLane {
             v[e / 2] = ptx::pack2(a, b);
         }
     }
-    // Address of a tensor's row 0 at the lane's first column, and from it that of row `row`: one instruction where the rows are
-    // one dimension.  `size`: of an element.
-    __device__ __forceinline__ char* base(const RowsPtr& t, int size) const { return t.p + (size_t)col(0, 0) * size; }
-    __device__ __forceinline__ static char* at(char* base, const RowsPtr& t, unsigned row, const RowNormParams& p) {
-        if (p.flat) return base + (size_t)row * (unsigned)t.row;
-        const unsigned b = row / p.T;
-        return base + (size_t)b * (size_t)t.batch + (size_t)(row - b * p.T) * (size_t)t.row;
+    // Address of row `row` of a tensor of T at the lane's first column.  SAME: all tensors share one 32-bit offset, and nothing but that
+    // is held for them ((16384, 1152) bf16: backward 60.8 -> 57.3 us; the forward with tangents 49.7 -> 58.3, so it has its own for each).
+    template <bool SAME>
+    __device__ __forceinline__ T* at(const RowsPtr& t, unsigned row, const RowNormParams& p) const {
+        if (SAME) return reinterpret_cast<T*>(t.p + (row * (unsigned)p.in[0].row + (unsigned)(col(0, 0) * (int)sizeof(T))));
+        return reinterpret_cast<T*>(row_of(t.p + col(0, 0) * (int)sizeof(T), t, row, p));
     }
 };
 
@@ -111,11 +118,11 @@ struct RowLane {
 // (16384, 1152) bf16: backward 67.8 -> 61.4 us, without tangents 39.2 -> 32.8, 8 bits 30.8 -> 28.4, norm of a sum 29.1 -> 28.6; not
 // with tangents in the forward, which has its bytes in flight (50.5 -> 57.7), nor for rows on warps ((131072, 128): 25.0 -> 26.1).
 // A row ahead in registers instead: 28.3 for the norm of a sum, 55 with tangents.
-template <int N, typename LANE>
+template <int N>
 __device__ __forceinline__ void row_prefetch(const RowNormParams& p, unsigned row, int bytes) {   // a thread for each tensor
     if (threadIdx.x < N && row < p.total) {
         const RowsPtr& t = p.in[threadIdx.x];
-        if (t.p) ptx::prefetch_l2(LANE::at(t.p, t, row, p), (uint32_t)bytes);
+        if (t.p) ptx::prefetch_l2(row_of(t.p, t, row, p), (uint32_t)bytes);
     }
 }
 
@@ -235,8 +242,6 @@ row_norm_kernel(const RowNormParams p) {
     const Lane L{BLOCK ? (int)threadIdx.x : lane & (p.P - 1), BLOCK ? (int)blockDim.x : p.P, p.D};
     const unsigned per_block = BLOCK ? 1u : (ROWNORM_THREADS / 32) * rpw;
     const float inv_d = 1.0f / (float)p.D;
-    char *x0 = L.base(p.in[0], E), *r0 = L.base(p.in[1], E), *tx0 = L.base(p.in[2], E), *tr0 = L.base(p.in[3], E);
-    char *y0 = L.base(p.out[0], MODE == ROW_S8 ? 1 : E), *h0 = L.base(p.out[1], E), *ty0 = L.base(p.out[2], E), *th0 = L.base(p.out[3], E);
     const bool res = p.in[1].p, tres = TAN && p.in[3].p;
     uint64_t g[C][V / 2];   // the same columns for every row
 #pragma unroll
@@ -246,24 +251,24 @@ row_norm_kernel(const RowNormParams p) {
         const unsigned row = BLOCK ? base : base + (threadIdx.x >> 5) * rpw + lane / p.P;
         const bool act = BLOCK || row < p.total;
         const unsigned at = act ? row : 0;
-        if (BLOCK && VEC && !TAN) row_prefetch<2, Lane>(p, row + gridDim.x, p.D * E);
+        if (BLOCK && VEC && !TAN) row_prefetch<2>(p, row + gridDim.x, p.D * E);
         uint64_t h[C][V / 2], t[TAN ? C : 1][V / 2];
         {
-            const T* x = reinterpret_cast<const T*>(Lane::at(x0, p.in[0], at, p));
+            const T* x = L.template at<false>(p.in[0], at, p);
             uint4 a[C], b[C], c[TAN ? C : 1], d[TAN ? C : 1];
 #pragma unroll
             for (int i = 0; i < C; ++i) a[i] = L.raw(x, act, i);
             if (res) {
-                const T* r = reinterpret_cast<const T*>(Lane::at(r0, p.in[1], at, p));
+                const T* r = L.template at<false>(p.in[1], at, p);
 #pragma unroll
                 for (int i = 0; i < C; ++i) b[i] = L.raw(r, act, i);
             }
             if constexpr (TAN) {
-                const T* tx = reinterpret_cast<const T*>(Lane::at(tx0, p.in[2], at, p));
+                const T* tx = L.template at<false>(p.in[2], at, p);
 #pragma unroll
                 for (int i = 0; i < C; ++i) c[i] = L.raw(tx, act, i);
                 if (tres) {
-                    const T* tr = reinterpret_cast<const T*>(Lane::at(tr0, p.in[3], at, p));
+                    const T* tr = L.template at<false>(p.in[3], at, p);
 #pragma unroll
                     for (int i = 0; i < C; ++i) d[i] = L.raw(tr, act, i);
                 }
@@ -274,7 +279,7 @@ row_norm_kernel(const RowNormParams p) {
                 if constexpr (TAN) rms_unpack(c[i], t[i]);
             }
             if (res) {
-                T* to = reinterpret_cast<T*>(Lane::at(h0, p.out[1], at, p));
+                T* to = L.template at<false>(p.out[1], at, p);
 #pragma unroll
                 for (int i = 0; i < C; ++i) {
                     uint64_t w[V / 2];
@@ -286,7 +291,7 @@ row_norm_kernel(const RowNormParams p) {
             }
             if constexpr (TAN)
                 if (tres) {
-                    T* to = reinterpret_cast<T*>(Lane::at(th0, p.out[3], at, p));
+                    T* to = L.template at<false>(p.out[3], at, p);
 #pragma unroll
                     for (int i = 0; i < C; ++i) {
                         uint64_t w[V / 2];
@@ -335,7 +340,7 @@ row_norm_kernel(const RowNormParams p) {
             const float k = fine ? __fdividef(127.f, top * up) : 0.f;
             if (act) {
                 if (L.c == 0) p.aux[row] = top * (p.norm ? inv : 1.f) * (1.f / 127.f);
-                int8_t* to = reinterpret_cast<int8_t*>(Lane::at(y0, p.out[0], at, p));
+                int8_t* to = reinterpret_cast<int8_t*>(row_of(p.out[0].p + L.col(0, 0), p.out[0], at, p));
                 const uint64_t up2 = ptx::pack2(up, up), k2 = ptx::pack2(k, k), round2 = ptx::pack2(12582912.f, 12582912.f);   // 1.5 2^23
 #pragma unroll
                 for (int i = 0; i < C; ++i) {
@@ -371,8 +376,8 @@ row_norm_kernel(const RowNormParams p) {
         } else if (act) {
             const float m = TAN ? sums[N - 1] * root * root * inv_d * pre : 0.f;   // (u . th) / (D r): th . h pre is known
             const uint64_t inv2 = ptx::pack2(inv, inv), nm2 = ptx::pack2(-m, -m);
-            T* y = reinterpret_cast<T*>(Lane::at(y0, p.out[0], at, p));
-            T* ty = TAN ? reinterpret_cast<T*>(Lane::at(ty0, p.out[2], at, p)) : nullptr;
+            T* y = L.template at<false>(p.out[0], at, p);
+            T* ty = TAN ? L.template at<false>(p.out[2], at, p) : nullptr;
 #pragma unroll
             for (int i = 0; i < C; ++i) {
                 uint64_t o[V / 2], u[V / 2];
@@ -398,7 +403,7 @@ row_norm_kernel(const RowNormParams p) {
 //     dg  = sum over the rows of dy u + dty J th
 // dx is the gradient of x and of the residual alike.  Every thread keeps the dg terms of its own columns over the rows it
 // walks; a block writes one row of partial sums, and a second kernel adds those up: fixed orders, the same bits each time.
-template <typename T, int C, bool BLOCK, bool VEC, bool TAN>
+template <typename T, int C, bool BLOCK, bool VEC, bool SAME, bool TAN>
 __global__ void __launch_bounds__(BLOCK ? rownorm_block_threads<T, C>() : ROWNORM_THREADS, rownorm_bwd_resident(BLOCK ? rownorm_block_threads<T, C>() : 0, TAN))
 row_norm_bwd_kernel(const RowNormParams p) {
     constexpr int V = RmsVec<T>::N, N = TAN ? 5 : 2, E = (int)sizeof(T);
@@ -413,8 +418,6 @@ row_norm_bwd_kernel(const RowNormParams p) {
     const Lane L{BLOCK ? (int)threadIdx.x : lane & (p.P - 1), BLOCK ? (int)blockDim.x : p.P, p.D};
     const unsigned per_block = BLOCK ? 1u : (ROWNORM_THREADS / 32) * rpw;
     const float inv_d = 1.0f / (float)p.D;
-    char *h0 = L.base(p.in[0], E), *y0 = L.base(p.in[1], E), *vh0 = L.base(p.in[2], E), *t0 = L.base(p.in[3], E), *z0 = L.base(p.in[4], E), *vt0 = L.base(p.in[5], E);
-    char *dx0 = L.base(p.out[0], E), *dt0 = L.base(p.out[1], E);
     const bool dh = p.in[2].p, dth = TAN && p.in[5].p;
     uint64_t held[RELOAD ? 1 : C][V / 2], dg[C][V / 2];   // the scale, and its gradient
 #pragma unroll
@@ -428,15 +431,14 @@ row_norm_bwd_kernel(const RowNormParams p) {
         const unsigned row = BLOCK ? base : base + warp * rpw + lane / p.P;
         const bool act = BLOCK || row < p.total;
         const unsigned at = act ? row : 0;
-        if (BLOCK && VEC) row_prefetch<TAN ? 6 : 3, Lane>(p, row + gridDim.x, p.D * E);
+        if (BLOCK && VEC) row_prefetch<TAN ? 6 : 3>(p, row + gridDim.x, p.D * E);
         // as loaded: half the registers that bf16 rows would take as fp32
         constexpr int H = RELOAD ? 1 : C, HT = RELOAD || !TAN ? 1 : C;
         uint4 hr[H], yr[H], tr[HT], zr[HT], vh[H], vt[HT];
         const T* from[6];
         {
-            char* const base[6] = {h0, y0, vh0, t0, z0, vt0};
 #pragma unroll
-            for (int k = 0; k < (TAN ? 6 : 3); ++k) from[k] = reinterpret_cast<const T*>(Lane::at(base[k], p.in[k], at, p));
+            for (int k = 0; k < (TAN ? 6 : 3); ++k) from[k] = L.template at<SAME>(p.in[k], at, p);
             auto load = [&](uint4* to, int k, bool there) {
 #pragma unroll
                 for (int i = 0; i < C; ++i) to[i] = L.raw(from[k], act && there, i);
@@ -513,8 +515,8 @@ row_norm_bwd_kernel(const RowNormParams p) {
         if (act) {
             const uint64_t inv2 = ptx::pack2(inv, inv), kh2 = ptx::pack2(kh, kh), kb2 = ptx::pack2(kb, kb), kt2 = ptx::pack2(kt, kt);
             const uint64_t zh2 = ptx::pack2(zh, zh), jt2 = ptx::pack2(jt, jt);
-            T* dx = reinterpret_cast<T*>(Lane::at(dx0, p.out[0], at, p));
-            T* dtx = TAN ? reinterpret_cast<T*>(Lane::at(dt0, p.out[1], at, p)) : nullptr;
+            T* dx = L.template at<SAME>(p.out[0], at, p);
+            T* dtx = TAN ? L.template at<SAME>(p.out[1], at, p) : nullptr;
 #pragma unroll
             for (int i = 0; i < C; ++i) {
                 uint64_t ox[V / 2], ot[V / 2], h[V / 2], y[V / 2], t[V / 2], z[V / 2], g[V / 2];

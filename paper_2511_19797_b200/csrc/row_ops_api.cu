@@ -63,7 +63,7 @@ struct RowsCall {
         esz = q.dtype == TVM_ATTN_FP32 ? 4 : 2;
         k.total = (unsigned)((long long)q.B * q.T);
         k.T = k.total;   // one dimension of rows, until a tensor needs two
-        k.flat = true;
+        k.flat = k.same = true;
         k.D = q.D;
         k.eps = q.eps;
         vec = q.D * esz % 16 == 0;
@@ -81,6 +81,8 @@ struct RowsCall {
         if (k.total <= 1) row = batch = p.D;
         if (row < p.D || batch < p.D || row > (1LL << 40) || batch > (1LL << 40) || reinterpret_cast<uintptr_t>(t->ptr) % size) { ok = false; return; }
         *to = {static_cast<char*>(t->ptr), row * size, batch * size};
+        // (8-bit rows have an offset of their own)
+        if (!eight && (row * size != k.in[0].row || (long long)k.total * row * size >= 1LL << 32 || (p.T > 1 && batch != row * p.T))) k.same = false;
         if (p.T > 1 && batch != row * p.T) { k.T = (unsigned)p.T; k.flat = false; }
         if (row * size >= 1LL << 32) k.flat = false;
         const long long unit = eight ? 8 : 16;
@@ -175,8 +177,9 @@ static int launch_norm_bwd(const RowsCall& c, float* dg, cudaStream_t st) {
     if (blocks > 0) {
         const int rc = with_row_split(split, [&](auto C, auto block) {
             const int threads = block() ? split.threads : ROWNORM_THREADS;
-            return c.vec ? launch(row_norm_bwd_kernel<T, C(), block(), true, TAN>, blocks, threads, 0, st, 0, k)
-                         : launch(row_norm_bwd_kernel<T, C(), block(), false, TAN>, blocks, threads, 0, st, 0, k);
+            return !c.vec ? launch(row_norm_bwd_kernel<T, C(), block(), false, false, TAN>, blocks, threads, 0, st, 0, k)
+                 : k.same ? launch(row_norm_bwd_kernel<T, C(), block(), true, true, TAN>, blocks, threads, 0, st, 0, k)
+                          : launch(row_norm_bwd_kernel<T, C(), block(), true, false, TAN>, blocks, threads, 0, st, 0, k);
         });
         if (rc != TVM_ATTN_OK) return rc;
     }

@@ -577,3 +577,21 @@ def test_offsets_beyond_32_bits(M):
     x = _draw(3, q.shape[0], K, dtype=torch.bfloat16).cuda()
     far.copy_(x)
     assert torch.equal(binding.tvm_attn_rmsnorm_jvp_fwd(far)[0], binding.tvm_attn_rmsnorm_jvp_fwd(x)[0])
+
+
+def test_backward_of_rows_beyond_32_bits():
+    """Two rows 4 GB apart, in all tensors or in some of them."""
+    D = 1152
+    buf = torch.empty((1 << 31) + 16 * D, dtype=torch.bfloat16, device="cuda")
+    near = [_draw(100 + k, 2, D, dtype=torch.bfloat16).cuda() for k in range(6)]
+    g = (1 + _draw(110, D, std=0.2)).cuda()
+    want = binding.tvm_attn_rmsnorm_jvp_bwd(*near, g)
+    far = [buf.as_strided((2, D), (1 << 31, 1), k * D) for k in range(8)]
+    for f, n in zip(far, near):
+        f.copy_(n)
+    for some in ((0, 1, 2, 3, 4, 5), (1,), (0, 3)):
+        got = binding.tvm_attn_rmsnorm_jvp_bwd(*(far[k] if k in some else near[k] for k in range(6)), g)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    dg = torch.empty_like(g)
+    got = binding.tvm_attn_rmsnorm_jvp_bwd(*far[:6], g, out=(far[6], far[7], dg))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
