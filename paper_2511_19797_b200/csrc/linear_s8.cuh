@@ -44,12 +44,13 @@ template <> __device__ __forceinline__ __nv_bfloat16 linear_round<__nv_bfloat16>
 // ------------------------------------------------------------------------------------------------ few rows
 constexpr int LIN_FEW_THREADS = 128, LIN_FEW_LOADS = 8;   // 16-byte loads of weights that a lane has in flight
 
-// 16 bytes of a row of k, zeros behind its end (the memory behind it is not read).
+// 16 bytes of a row of k, zeros behind its end (the memory behind it is not read).  (No loads by the read-only path in these kernels: they are
+// set up while the kernel in front of them may still write what they read.)
 __device__ __forceinline__ uint4 linear_load16(const int8_t* row, int k, int K, bool stream) {
     uint4 v = make_uint4(0, 0, 0, 0);
     if (k + 16 <= K) {
-        if (stream) asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + k));
-        else v = __ldg(reinterpret_cast<const uint4*>(row + k));
+        if (stream) asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + k));
+        else v = *reinterpret_cast<const uint4*>(row + k);
     } else if (k < K) {
         uint32_t b[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -233,13 +234,13 @@ __device__ __forceinline__ void linear_store(const LinearParams& p, const LinBlo
         int tm, tn;
         linear_tile(p, tile, tm, tn);
         const long long m = (long long)tm * 2 * LIN_ROWS + k.rank * LIN_ROWS + quad * 32 + lane;
-        sm = m < p.M ? __ldg(p.s + m) : 0.f;
+        sm = m < p.M ? p.s[m] : 0.f;
 #pragma unroll
         for (int j = 0; j < COLS; ++j) {
             const int at = 32 * j + lane, unit = 2 * (at / C::UNIT) + ((side + n) & 1), col = tn * BN + unit * C::UNIT + at % C::UNIT;
             const bool in = unit < C::UNITS && col < p.N;
-            wsc[j] = in ? __ldg(p.ws + col) : 0.f;
-            bia[j] = in && p.bias ? __ldg(p.bias + col) : 0.f;
+            wsc[j] = in ? p.ws[col] : 0.f;
+            bia[j] = in && p.bias ? p.bias[col] : 0.f;
         }
     };
     fetch(pair, 0);
@@ -470,7 +471,7 @@ linear_s8_thin_kernel(const __grid_constant__ CUtensorMap mw, const __grid_const
     bool ok = !skip && warp >= 2 && ptx::mbar_wait_warp_s(done, 0, flag_addr, LIN_WAIT_LIMIT_NS);
     if (ok) ptx::tc_fence_after_sync();
     const bool in = ok && n < p.N;
-    const float wsc = in ? __ldg(p.ws + n) : 0.f, bias = in && p.bias ? __ldg(p.bias + n) : 0.f;
+    const float wsc = in ? p.ws[n] : 0.f, bias = in && p.bias ? p.bias[n] : 0.f;
     auto store = [&](int m, int sum, float sm) { static_cast<OUT*>(p.y)[m * p.ldy + n] = linear_round<OUT>(fmaf((float)sum * sm, wsc, bias)); };
     // Each CTA adds up the same number of tokens, four by four: the sums of four tokens and a channel are 16 bytes of each CTA's.
     const int quads = ((p.M + 3) / 4 + parts - 1) / parts;
@@ -491,7 +492,7 @@ linear_s8_thin_kernel(const __grid_constant__ CUtensorMap mw, const __grid_const
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (c + j + e < p.M && in) store(c + j + e, (int)r[j + e], __ldg(p.s + c + j + e));
+                        if (c + j + e < p.M && in) store(c + j + e, (int)r[j + e], p.s[c + j + e]);
                 }
             }
         }
@@ -504,7 +505,7 @@ linear_s8_thin_kernel(const __grid_constant__ CUtensorMap mw, const __grid_const
         const int m0 = part * quads * 4;   // the first of this CTA's tokens
         for (int i0 = 0; i0 < quads && m0 + 4 * i0 < p.M; i0 += 8) {
             // the scales of the next 32 tokens, a lane each
-            const float sv = m0 + 4 * i0 + lane < p.M ? __ldg(p.s + m0 + 4 * i0 + lane) : 0.f;
+            const float sv = m0 + 4 * i0 + lane < p.M ? p.s[m0 + 4 * i0 + lane] : 0.f;
 #pragma unroll 2
             for (int i = 0; i < 8; ++i) {
                 if (i0 + i >= quads) break;

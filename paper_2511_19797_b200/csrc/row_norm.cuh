@@ -41,13 +41,14 @@ constexpr int ROWNORM_SINGLE = 160;    // chunks of a row with one on each threa
 // Threads that a block with one row can have, C chunks each.
 template <typename T, int C> constexpr int rownorm_block_threads() { return C == 4 && sizeof(T) == 4 ? 1024 : C == 1 ? ROWNORM_SINGLE : 512; }
 // Blocks of the backward on an SM: as many as the registers let in (a block walks over its rows from the start to the end of the
-// launch, so one that waits for another's end would double the time).  `threads`: of a block with one row, 0 for rows on warps.
-__host__ __device__ constexpr int rownorm_bwd_resident(int threads, bool tan) {
-    return threads == 0 ? (tan ? 2 : 4) : threads <= 160 ? (tan ? 4 : 7) : threads <= 256 ? 2 : 1;
+// launch, so one that waits for another's end would double the time).  `threads`: of a block with one row of C chunks a thread, 0 for
+// rows on warps.
+__host__ __device__ constexpr int rownorm_bwd_resident(int threads, int C, bool tan) {
+    return threads == 0 ? (tan ? 2 : 4) : C == 1 ? (tan ? 4 : 7) : threads <= 512 ? 512 / threads : 1;
 }
 // All of them.  A fixed number: the partial sums of the scale's gradient, a row per block, have a size and an order that do not
 // depend on the device.
-__host__ __device__ constexpr int rownorm_bwd_blocks(int threads, bool tan) { return 148 * rownorm_bwd_resident(threads, tan); }
+__host__ __device__ constexpr int rownorm_bwd_blocks(int threads, int C, bool tan) { return 148 * rownorm_bwd_resident(threads, C, tan); }
 
 // `base` moved on by `row` rows of tensor t: one instruction where the rows are one dimension.
 __device__ __forceinline__ char* row_of(char* base, const RowsPtr& t, unsigned row, const RowNormParams& p) {
@@ -99,8 +100,8 @@ struct RowLane {
         for (int e = 0; e < V; e += 2) {
             float a = 1.f, b = 1.f;
             if (g) {
-                a = col(i, e) < D ? __ldg(g + col(i, e)) : 0.f;
-                b = col(i, e + 1) < D ? __ldg(g + col(i, e + 1)) : 0.f;
+                a = col(i, e) < D ? g[col(i, e)] : 0.f;
+                b = col(i, e + 1) < D ? g[col(i, e + 1)] : 0.f;
             }
             v[e / 2] = ptx::pack2(a, b);
         }
@@ -404,7 +405,7 @@ row_norm_kernel(const RowNormParams p) {
 // dx is the gradient of x and of the residual alike.  Every thread keeps the dg terms of its own columns over the rows it
 // walks; a block writes one row of partial sums, and a second kernel adds those up: fixed orders, the same bits each time.
 template <typename T, int C, bool BLOCK, bool VEC, bool SAME, bool TAN>
-__global__ void __launch_bounds__(BLOCK ? rownorm_block_threads<T, C>() : ROWNORM_THREADS, rownorm_bwd_resident(BLOCK ? rownorm_block_threads<T, C>() : 0, TAN))
+__global__ void __launch_bounds__(BLOCK ? rownorm_block_threads<T, C>() : ROWNORM_THREADS, rownorm_bwd_resident(BLOCK ? rownorm_block_threads<T, C>() : 0, C, TAN))
 row_norm_bwd_kernel(const RowNormParams p) {
     constexpr int V = RmsVec<T>::N, N = TAN ? 5 : 2, E = (int)sizeof(T);
     // Rows of four chunks a thread are read again, from L1 and L2, for the outputs: held, they and the scale would not fit into
@@ -583,7 +584,7 @@ row_norm_bwd_kernel(const RowNormParams p) {
 
 // dg[j] = sum over the n partial rows, in a fixed order: 8 columns a block, the rows over 128 threads.  Launched as a programmatic
 // dependent of the kernel above.  n = 0 (no rows at all) gives zeros.
-__global__ void __launch_bounds__(1024) row_norm_dg_kernel(const float* __restrict__ partial, float* __restrict__ dg, int n, int D) {
+__global__ void __launch_bounds__(1024) row_norm_dg_kernel(const float* partial, float* dg, int n, int D) {
     __shared__ float acc[32][8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 8 + (lane & 7);
     ptx::dependency_wait();

@@ -165,7 +165,7 @@ static int launch_norm(const RowsCall& c, cudaStream_t st) {
 
 static int bwd_blocks(const RowSplit& split, bool tan, long long rows) {
     const int per_block = split.threads ? 1 : ROWNORM_THREADS / 32 * (32 / split.P);
-    return (int)fewer((rows + per_block - 1) / per_block, rownorm_bwd_blocks(split.threads, tan));
+    return (int)fewer((rows + per_block - 1) / per_block, rownorm_bwd_blocks(split.threads, split.C, tan));
 }
 
 template <typename T, bool TAN>
@@ -188,7 +188,7 @@ static int launch_norm_bwd(const RowsCall& c, float* dg, cudaStream_t st) {
 
 static size_t norm_bwd_workspace(const tvm_attn_rows_params& p) {
     const RowSplit split = row_split(p.D, p.dtype == TVM_ATTN_FP32 ? 4 : 2, ROWNORM_SINGLE);
-    const int tan = rownorm_bwd_blocks(split.threads, true), plain = rownorm_bwd_blocks(split.threads, false);
+    const int tan = rownorm_bwd_blocks(split.threads, split.C, true), plain = rownorm_bwd_blocks(split.threads, split.C, false);
     return (size_t)(tan > plain ? tan : plain) * (size_t)p.D * sizeof(float);
 }
 
@@ -330,9 +330,10 @@ static int launch_many(LinearParams p, const DeviceFacts& dev, cudaStream_t st) 
     return launch(kern, 2 * fewer(tiles, dev.sms / 2), LIN_THREADS, C::SMEM_BYTES, st, 0, ma, mb, my, p);
 }
 
-// Cycles of a product in tiles of 256 rows, and the width of a tile: the one whose rounds of tiles take least.  What an SM loads bounds
-// them (62 bytes a cycle from L2, 128 + BN / 2 rows of k for each of a pair's CTAs: 446 cycles per 128 bytes of k at 192 channels, 402 at
-// 128), not its MMAs.  -1: more tiles than there can be.
+// Cycles of a product in tiles of 256 rows, and the width of a tile: the one whose rounds of tiles take least.  Narrow tiles load more for what
+// they compute: 128 bytes of k took 776, 624, 546 and 484 cycles with 256, 192, 128 and 64 channels (K = 9216, four tiles a pair, of a clock that the power
+// cap lowers), in proportion to 256 + BN.  16384 x 3456 x 1152 51.9, 54.4, 65.8, 109.8 us; 8000 x 768 x 768 10.5, 9.6, 10.8, 15.6; 512 x 4608 x 1152 9.5,
+// 8.5, 7.6, 11.0.  -1: more tiles than there can be.
 static long long many_cycles(const LinearParams& p, const DeviceFacts& dev, int* width) {
     const long long tiles_m = (p.M + 2 * LIN_ROWS - 1) / (2 * LIN_ROWS), pairs = dev.sms / 2, kblocks = (p.K + 127) / 128;
     if (tiles_m * ((p.N + 63) / 64) > 2147483647LL) return -1;
@@ -369,7 +370,7 @@ static int linear_thin(const LinearParams& p, const DeviceFacts& dev, cudaStream
     return p.M <= 128 ? launch_thin<128, OUT>(p, dev, st) : launch_thin<256, OUT>(p, dev, st);
 }
 
-// Cycles of a product on linear_s8_thin_kernel, by its number of CTAs that share k: an SM's CTAs share its loads (62 bytes a cycle) and the
+// Cycles of a product on linear_s8_thin_kernel, by its number of CTAs that share k: an SM's CTAs share its loads (some 64 bytes a cycle) and the
 // writes of their sums (26 cycles a token), and add up some tokens each (125 cycles a token).
 static long long thin_cycles(const LinearParams& p, const DeviceFacts& dev, int split) {
     const int NT = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : p.M <= 128 ? 128 : 256;

@@ -520,7 +520,7 @@ def test_captured_calls_replay_bit_for_bit():
 def test_calls_in_a_row_wait_for_one_another():
     """Kernels are set up while the one in front of them ends: the same buffers written and read by call after call."""
     w, ws = binding.tvm_attn_quantize_s8(_draw(90, 640, 1152).cuda())
-    for rows in (5, 100, 3000):
+    for rows in (1, 2, 5, 100, 3000):
         xs = [_draw(91 + k, rows, 1152, dtype=torch.bfloat16).cuda() for k in range(4)]
         want = []
         for x in xs:
