@@ -595,3 +595,51 @@ def test_backward_of_rows_beyond_32_bits():
     dg = torch.empty_like(g)
     got = binding.tvm_attn_rmsnorm_jvp_bwd(*far[:6], g, out=(far[6], far[7], dg))
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_calls_from_several_threads_next_to_the_attention():
+    """Host threads with a stream each: norms and products of every kind, and attention, whose kernels take the same tensor memory."""
+    import threading
+    args = _graph_inputs()
+    Q, K, V, tQ, tK, tV = (_draw(120 + k, 2, 4, 600, 64, dtype=torch.bfloat16).cuda() for k in range(6))
+
+    def attention():
+        saved = binding.tvm_attn_jvp_fwd(Q, K, V, tQ, tK, tV)
+        return tuple(saved) + tuple(binding.tvm_attn_jvp_bwd(Q, K, V, tQ, tK, tV, *saved, Q, tQ))
+
+    def products():
+        q, s = binding.tvm_attn_quantize_s8(args[0])
+        return tuple(binding.tvm_attn_linear_s8(q[:m], s[:m], args[2], args[3]) for m in (1, 2, 16, 60, 130, 250, 700))
+
+    jobs = [attention, products, lambda: _everything(*args), products]
+    want = [job() for job in jobs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                got = jobs[i]()
+                torch.cuda.current_stream().synchronize()
+                wrong.extend((i, k) for k, (a, b) in enumerate(zip(got, want[i])) if not torch.equal(a, b))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(jobs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong[:5]
+    binding.tvm_attn_check_status()
+
+
+def test_a_first_call_under_capture():
+    """A kernel's first launch may come inside a capture: shapes that no test before has used choose their kernels there."""
+    (_, q), (_, w) = _rows8(1, 500, 272), _rows8(2, 330, 272)
+    s, ws, x = torch.ones(500, device="cuda"), torch.ones(330, device="cuda"), _draw(3, 90, 2600, dtype=torch.bfloat16).cuda()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = [binding.tvm_attn_linear_s8(q[:m], s[:m], w, ws, dtype=torch.float32) for m in (1, 30, 500)] + [binding.tvm_attn_rmsnorm_jvp_bwd(x, x, x, x)[0]]
+    graph.replay()
+    torch.cuda.synchronize()
+    want = [binding.tvm_attn_linear_s8(q[:m], s[:m], w, ws, dtype=torch.float32) for m in (1, 30, 500)] + [binding.tvm_attn_rmsnorm_jvp_bwd(x, x, x, x)[0]]
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
