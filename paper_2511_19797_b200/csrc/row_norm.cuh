@@ -96,6 +96,16 @@ struct RowLane {
     }
     // The scale's elements for a chunk: 1 where there is no scale, 0 behind the row.
     __device__ __forceinline__ void scale(const float* g, int i, uint64_t (&v)[V / 2]) const {
+        if (VEC && g) {   // (the scale is aligned too, and whole chunks stand in a row or behind it)
+#pragma unroll
+            for (int e = 0; e < V / 2; e += 2) {
+                float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (col(i, 0) < D) q = *reinterpret_cast<const float4*>(g + col(i, 2 * e));
+                v[e] = ptx::pack2(q.x, q.y);
+                v[e + 1] = ptx::pack2(q.z, q.w);
+            }
+            return;
+        }
 #pragma unroll
         for (int e = 0; e < V; e += 2) {
             float a = 1.f, b = 1.f;
@@ -408,9 +418,9 @@ template <typename T, int C, bool BLOCK, bool VEC, bool SAME, bool TAN>
 __global__ void __launch_bounds__(BLOCK ? rownorm_block_threads<T, C>() : ROWNORM_THREADS, rownorm_bwd_resident(BLOCK ? rownorm_block_threads<T, C>() : 0, C, TAN))
 row_norm_bwd_kernel(const RowNormParams p) {
     constexpr int V = RmsVec<T>::N, N = TAN ? 5 : 2, E = (int)sizeof(T);
-    // Rows of four chunks a thread are read again, from L1 and L2, for the outputs: held, they and the scale would not fit into
-    // registers ((1024, 16384) bf16 with tangents 202 -> 106 us).
-    constexpr bool RELOAD = C > 2;
+    // Rows of four chunks a thread, with tangents of two, are read again, from L1 and L2, for the outputs: held, they cost more warps than that
+    // ((1024, 16384) bf16 with tangents 202 -> 106 us, (4096, 4096) 59 -> 56.5; without tangents 32.5 -> 36.8, one chunk with them 54.6 -> 59).
+    constexpr bool RELOAD = C > (TAN ? 1 : 2), HOLD_G = C <= 2;
     ptx::dependency_wait();
     __shared__ __align__(16) float slots[BLOCK ? 2 * 32 * N : 32 * V];
     if constexpr (BLOCK) clear_slots(slots, 2 * 32 * N);
@@ -420,10 +430,10 @@ row_norm_bwd_kernel(const RowNormParams p) {
     const unsigned per_block = BLOCK ? 1u : (ROWNORM_THREADS / 32) * rpw;
     const float inv_d = 1.0f / (float)p.D;
     const bool dh = p.in[2].p, dth = TAN && p.in[5].p;
-    uint64_t held[RELOAD ? 1 : C][V / 2], dg[C][V / 2];   // the scale, and its gradient
+    uint64_t held[HOLD_G ? C : 1][V / 2], dg[C][V / 2];   // the scale, and its gradient
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-        if constexpr (!RELOAD) L.scale(p.g, i, held[i]);
+        if constexpr (HOLD_G) L.scale(p.g, i, held[i]);
 #pragma unroll
         for (int e = 0; e < V / 2; ++e) dg[i][e] = 0ull;
     }
@@ -456,13 +466,16 @@ row_norm_bwd_kernel(const RowNormParams p) {
                 rms_unpack(L.raw(from[0], act, i), h);
                 rms_unpack(L.raw(from[1], act, i), y);
                 if constexpr (TAN) { rms_unpack(L.raw(from[3], act, i), t); rms_unpack(L.raw(from[4], act, i), z); }
-                L.scale(p.g, i, g);
             } else {
                 rms_unpack(hr[i], h);
                 rms_unpack(yr[i], y);
                 if constexpr (TAN) { rms_unpack(tr[i], t); rms_unpack(zr[i], z); }
+            }
+            if constexpr (HOLD_G) {
 #pragma unroll
                 for (int e = 0; e < V / 2; ++e) g[e] = held[i][e];
+            } else {
+                L.scale(p.g, i, g);
             }
         };
         // Ends the reuse of an earlier unpacking across the reductions.
@@ -582,25 +595,26 @@ row_norm_bwd_kernel(const RowNormParams p) {
     }
 }
 
-// dg[j] = sum over the n partial rows, in a fixed order: 8 columns a block, the rows over 128 threads.  Launched as a programmatic
-// dependent of the kernel above.  n = 0 (no rows at all) gives zeros.
+// dg[j] = sum over the n partial rows, in a fixed order: COLS columns a block, the rows over 1024 / COLS threads.  Launched as a
+// programmatic dependent of the kernel above.  n = 0 (no rows at all) gives zeros.
+template <int COLS>
 __global__ void __launch_bounds__(1024) row_norm_dg_kernel(const float* partial, float* dg, int n, int D) {
-    __shared__ float acc[32][8];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 8 + (lane & 7);
+    __shared__ float acc[32][COLS + 1];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * COLS + (lane & (COLS - 1));
     ptx::dependency_wait();
     float v = 0.f;
     if (j < D) {
 #pragma unroll 8
-        for (int b = threadIdx.x >> 3; b < n; b += 128) v += partial[(size_t)b * D + j];
+        for (int b = threadIdx.x / COLS; b < n; b += 1024 / COLS) v += partial[(size_t)b * D + j];
     }
-    v += __shfl_xor_sync(0xffffffffu, v, 8);
-    v += __shfl_xor_sync(0xffffffffu, v, 16);
-    if (lane < 8) acc[warp][lane] = v;
+#pragma unroll
+    for (int off = COLS; off < 32; off <<= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    if (lane < COLS) acc[warp][lane] = v;
     __syncthreads();
-    if (warp < 8) {   // a column each
+    if (warp < COLS) {   // a column each
         v = acc[lane][warp];
         for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-        if (lane == 0 && blockIdx.x * 8 + warp < D) dg[blockIdx.x * 8 + warp] = v;
+        if (lane == 0 && blockIdx.x * COLS + warp < D) dg[blockIdx.x * COLS + warp] = v;
     }
 }
 

@@ -183,7 +183,10 @@ static int launch_norm_bwd(const RowsCall& c, float* dg, cudaStream_t st) {
         });
         if (rc != TVM_ATTN_OK) return rc;
     }
-    return dg ? launch(row_norm_dg_kernel, (unsigned)(k.D + 7) / 8, 1024, 0, st, 0, k.aux, dg, blocks, k.D) : TVM_ATTN_OK;
+    if (!dg) return TVM_ATTN_OK;
+    // as few columns a block as leave no SM without one: 8 are a sector of each partial row, 32 a line
+    if (k.D <= 8 * 148) return launch(row_norm_dg_kernel<8>, (unsigned)(k.D + 7) / 8, 1024, 0, st, 0, k.aux, dg, blocks, k.D);
+    return launch(row_norm_dg_kernel<32>, (unsigned)(k.D + 31) / 32, 1024, 0, st, 0, k.aux, dg, blocks, k.D);
 }
 
 static size_t norm_bwd_workspace(const tvm_attn_rows_params& p) {
