@@ -13,6 +13,9 @@
 // operand with 128 rows, and the CTAs of a cluster share k.  Up to 2 rows (single tokens) dp4a on operands that go from global memory
 // straight to registers keeps pace with HBM: nothing is set up, and nothing waits.  (mma.sync, which emulates 8-bit products on this
 // GPU at some 150 multiply-adds a cycle and SM, took 20 us for one token and 14336 x 4096 weights.)
+//
+// Measured on B200: 16384 x 3456 x 1152, bf16 out, 52 us in bursts and 61 at the power cap (2.1 Pop/s), 16384 x 4608 x 9216 421 (3.3 Pop/s, bursts), output
+// alone (K = 128) at the rate of a fill; one token against 14336 x 4096 11.6 us (5 TB/s), 28672 x 4096 20.3 (5.8), 16 tokens 14.3, 64 tokens 18.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>

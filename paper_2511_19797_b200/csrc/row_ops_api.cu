@@ -387,7 +387,7 @@ static int linear(LinearParams p, cudaStream_t st) {
     const int rc = tensor_core_device(&dev);
     if (rc != TVM_ATTN_OK) return rc;
     // One or two tokens on dp4a, unless the products are so long that they take longer than the weights' bytes.  14336 x 4096 weights, one
-    // token 12.3 us (16.5 on the tensor cores), two 13.6; 4096 x 14336 one 14.0 (16.5), two 17.9 (16.5).
+    // token 11.6 us (13.7 on the tensor cores), two 12.3; 4096 x 14336 one 12.9 (14.7), two 17.9 (14.5).
     if (p.M <= 2 && (long long)p.M * p.K <= 16384) return p.M == 1 ? linear_few<OUT, 1>(p, st) : linear_few<OUT, 2>(p, st);
     int bn = 0;
     const long long many = many_cycles(p, *dev, &bn);
