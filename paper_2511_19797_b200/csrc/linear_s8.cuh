@@ -317,22 +317,31 @@ __device__ __forceinline__ void linear_store(const LinearParams& p, const LinBlo
                     if (row0 < p.M && col0 < p.N) ptx::tma_store_2d(&my, to, col0, (int)row0);
                     ptx::bulk_commit();
                 }
-            } else {   // rows that do not begin or end on 16 bytes: a warp stores one row after the other
+            } else {   // rows that do not begin or end on 16 bytes: a warp stores one row after the other, 4 bytes a lane if they begin on 4
                 __syncwarp();
-                for (int i = 0; i < 32 && row0 + i < p.M; ++i) {
-                    OUT* dst = static_cast<OUT*>(p.y) + (row0 + i) * p.ldy + col0;
+                const long long rows = p.M - row0;
+                const int cols = p.N - col0;
+                OUT* dst = static_cast<OUT*>(p.y) + row0 * p.ldy + col0;
+                auto staged = [&](int i, int c) { return to + i * 128 + (((c / PER16) ^ (i & 7)) << 4) + c % PER16 * (int)sizeof(OUT); };
+                if (sizeof(OUT) == 4 || ((reinterpret_cast<uintptr_t>(p.y) | (uintptr_t)(p.ldy * 2)) & 3) == 0) {
+                    constexpr int E = 4 / (int)sizeof(OUT);   // elements of 4 bytes
+#pragma unroll 8
+                    for (int i = 0; i < 32; ++i) {
+                        uint32_t v;
+                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(staged(i, E * lane)));
+                        OUT* at = dst + i * p.ldy + E * lane;
+                        if (i < rows && E * lane + E <= cols) *reinterpret_cast<uint32_t*>(at) = v;
+                        else if (i < rows && E * lane < cols) *reinterpret_cast<unsigned short*>(at) = (unsigned short)v;   // (a last odd column)
+                    }
+                } else {
+#pragma unroll 8
+                    for (int i = 0; i < 32; ++i) {
+                        unsigned short v[2];
 #pragma unroll
-                    for (int c = lane; c < C::UNIT; c += 32) {
-                        const uint32_t at = to + i * 128 + (((c / PER16) ^ (i & 7)) << 4) + c % PER16 * (int)sizeof(OUT);
-                        if constexpr (sizeof(OUT) == 2) {
-                            unsigned short v;
-                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
-                            if (col0 + c < p.N) *reinterpret_cast<unsigned short*>(dst + c) = v;
-                        } else {
-                            float v;
-                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
-                            if (col0 + c < p.N) dst[c] = v;
-                        }
+                        for (int h = 0; h < 2; ++h) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v[h]) : "r"(staged(i, lane + 32 * h)));
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            if (i < rows && lane + 32 * h < cols) *reinterpret_cast<unsigned short*>(dst + i * p.ldy + lane + 32 * h) = v[h];
                     }
                 }
                 __syncwarp();
