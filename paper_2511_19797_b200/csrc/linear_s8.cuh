@@ -125,7 +125,7 @@ struct LinCfg {
     static constexpr int A_BYTES = LIN_ROWS * 128, B_BYTES = BN / 2 * 128, STAGE = A_BYTES + B_BYTES;
     // The epilogue works on units of 128 bytes of 32 rows, which its eight warps, two for each 32 rows of the accumulator, take in turn.
     static constexpr int UNIT = 128 / (int)sizeof(OUT), UNITS = BN / UNIT, WARP_UNITS = (UNITS + 1) / 2, UNIT_BYTES = 32 * 128;
-    static constexpr int BUFS = 1, STAGING = 8 * BUFS * UNIT_BYTES, WARP_COLS = WARP_UNITS * UNIT, TABLES = 8 * 2 * WARP_COLS * 4;
+    static constexpr int STAGING = 8 * UNIT_BYTES, WARP_COLS = WARP_UNITS * UNIT, TABLES = 8 * 2 * WARP_COLS * 4;
     static constexpr int BARRIERS = 256, MOST = 227 * 1024 - 1024;
     static constexpr int STAGES = (MOST - STAGING - TABLES - BARRIERS) / STAGE < 8 ? (MOST - STAGING - TABLES - BARRIERS) / STAGE : 8;
     static constexpr int O_STAGING = STAGES * STAGE, O_TABLES = O_STAGING + STAGING, O_BARRIERS = O_TABLES + TABLES;
@@ -227,7 +227,7 @@ __device__ __forceinline__ void linear_store(const LinearParams& p, const LinBlo
     using C = LinCfg<BN, OUT>;
     constexpr int PER16 = 16 / (int)sizeof(OUT), COLS = (C::WARP_COLS + 31) / 32;
     const int tiles = p.tiles_m * p.tiles_n, lane = threadIdx.x & 31, warp = threadIdx.x / 32 - 4, quad = warp & 3, side = warp >> 2;
-    const uint32_t staging = k.base + C::O_STAGING + warp * C::BUFS * C::UNIT_BYTES, table = k.base + C::O_TABLES + warp * 2 * C::WARP_COLS * 4;
+    const uint32_t to = k.base + C::O_STAGING + warp * C::UNIT_BYTES, table = k.base + C::O_TABLES + warp * 2 * C::WARP_COLS * 4;
     const uint32_t acc_empty = ptx::cluster_address(k.acc_empty(0), 0);
     // A tile's scales: the lane's row's, and those and the biases of the columns of the warp's units (unit 2 j + its turn), a lane's
     // share of them.  They are loaded a tile ahead and handed out through a table of the warp's own.
@@ -247,7 +247,6 @@ __device__ __forceinline__ void linear_store(const LinearParams& p, const LinBlo
         }
     };
     fetch(pair, 0);
-    uint32_t buf = 0;
     int n = 0;
     for (int tile = pair; tile < tiles; tile += pairs, ++n) {
         int tm, tn;
@@ -282,8 +281,7 @@ __device__ __forceinline__ void linear_store(const LinearParams& p, const LinBlo
                 if (lane == 0) ptx::mbar_arrive_cluster(acc_empty + 8 * acc);
             }
             if (!there) break;
-            const uint32_t to = staging + buf * C::UNIT_BYTES;
-            if (lane == 0) ptx::bulk_wait_read<C::BUFS - 1>();   // the store that read this buffer last is done with it
+            if (lane == 0) ptx::bulk_wait_read();   // the store before is done with the staged unit
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {   // pieces of 16 bytes
@@ -346,7 +344,6 @@ __device__ __forceinline__ void linear_store(const LinearParams& p, const LinBlo
                 }
                 __syncwarp();
             }
-            buf = C::BUFS == 2 ? buf ^ 1 : 0;
             if (last) break;
         }
     }
