@@ -643,3 +643,25 @@ def test_a_first_call_under_capture():
     torch.cuda.synchronize()
     want = [binding.tvm_attn_linear_s8(q[:m], s[:m], w, ws, dtype=torch.float32) for m in (1, 30, 500)] + [binding.tvm_attn_rmsnorm_jvp_bwd(x, x, x, x)[0]]
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [72, 333, 1152, 2560, 8192, 16384])
+def test_in_place_at_every_split_of_a_row(D, dtype):
+    """Outputs over each of the inputs in turn, several rows a block."""
+    rows, g = 1500 if D < 3000 else 300, (1 + _draw(9, D, std=0.2)).cuda()
+    src = [_draw(130 + k, rows, D, dtype=dtype).cuda() for k in range(6)]
+    want = binding.tvm_attn_rmsnorm_jvp_bwd(*src, g)
+    for a, b in ((0, 2), (1, 3), (2, 0), (4, 5), (5, 4), (3, 1)):
+        t = [v.clone() for v in src]
+        got = binding.tvm_attn_rmsnorm_jvp_bwd(*t, g, out=(t[a], t[b], torch.empty_like(g)))
+        assert all(torch.equal(x, y) for x, y in zip(got, want)), (a, b)
+    want = binding.tvm_attn_rmsnorm_jvp_fwd(*src[:4], g)
+    for order in ((0, 1, 2, 3), (3, 2, 1, 0), (1, 0, 3, 2), (2, 3, 0, 1)):
+        t = [v.clone() for v in src[:4]]
+        got = binding.tvm_attn_rmsnorm_jvp_fwd(*t, g, out=[t[k] for k in order])
+        assert all(torch.equal(x, y) for x, y in zip(got, want)), order
+    q, s, h = binding.tvm_attn_rmsnorm_s8(*src[:2], g)
+    t = [v.clone() for v in src[:2]]
+    got = binding.tvm_attn_rmsnorm_s8(*t, g, out=(torch.empty_like(q), torch.empty_like(s), t[0]))
+    assert torch.equal(got[0], q) and torch.equal(got[1], s) and torch.equal(t[0], h)
