@@ -197,7 +197,8 @@ int tvm_qk_rmsnorm_jvp_bwd(const tvm_attn_params* p, float eps, const void* Q, c
  * strides of its own.  A null tvm_attn_rows* or a null ptr in it is an absent tensor.  Rows that begin on 16 bytes (pointer
  * and strides multiples of 16 bytes, and of 8 for 8-bit rows; D a multiple of 16 bytes; a 16-byte aligned scale) are read and
  * written 16 bytes at a time, others element by element (and their sums added up in another order).  Pointers are aligned to their element.
- * An output may be one of the call's inputs of the same type, with the same strides; otherwise outputs overlap nothing.
+ * An output may be one of the call's inputs of the same type, with the same strides; otherwise outputs overlap nothing (those that begin
+ * where another output does, or where an input does that lies differently, are TVM_ATTN_INVALID_ARG).
  * B = 0 or T = 0 is a call without rows (TVM_ATTN_OK).
  */
 #define TVM_ATTN_MAX_WIDTH 16384

@@ -88,6 +88,19 @@ struct RowsCall {
         const long long unit = eight ? 8 : 16;
         vec = vec && reinterpret_cast<uintptr_t>(t->ptr) % unit == 0 && row * size % unit == 0 && batch * size % unit == 0;
     }
+    // Outputs that begin where another output does, or where an input does that lies differently, would be read or written by two
+    // threads.  (Other overlaps are the caller's to avoid.)  `eight`: the first output is 8-bit rows, which lie differently from all inputs.
+    bool overlapping(bool eight = false) const {
+        for (int i = 0; i < 4; ++i) {
+            const RowsPtr& o = k.out[i];
+            if (!o.p) continue;
+            for (int j = 0; j < i; ++j)
+                if (k.out[j].p == o.p) return true;
+            for (const RowsPtr& x : k.in)
+                if (x.p == o.p && ((eight && i == 0) || x.row != o.row || x.batch != o.batch)) return true;
+        }
+        return false;
+    }
     void scale(const float* g) {
         k.g = g;
         ok = ok && reinterpret_cast<uintptr_t>(g) % 4 == 0;
@@ -212,7 +225,7 @@ int tvm_attn_rmsnorm_jvp_fwd(const tvm_attn_rows_params* p, const tvm_attn_rows*
     c.add(x, &c.k.in[0], true); c.add(res, &c.k.in[1], false); c.add(tx, &c.k.in[2], false); c.add(tres, &c.k.in[3], false);
     c.add(y, &c.k.out[0], true); c.add(h, &c.k.out[1], false); c.add(ty, &c.k.out[2], false); c.add(th, &c.k.out[3], false);
     c.scale(g);
-    if (!c.ok) return TVM_ATTN_INVALID_ARG;
+    if (!c.ok || c.overlapping()) return TVM_ATTN_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     return present(tx) ? launch_norm<ROW_NORM_TAN>(c, st) : launch_norm<ROW_NORM>(c, st);
 }
@@ -236,7 +249,7 @@ int tvm_attn_rmsnorm_jvp_bwd(const tvm_attn_rows_params* p, const tvm_attn_rows*
         c.add(th, &c.k.in[3], false); c.add(dty, &c.k.in[4], false); c.add(dth, &c.k.in[5], false);
         c.add(dx, &c.k.out[0], true); c.add(dtx, &c.k.out[1], false);
     }
-    if (!c.ok) return TVM_ATTN_INVALID_ARG;
+    if (!c.ok || c.overlapping()) return TVM_ATTN_INVALID_ARG;
     if (g) {
         if (!workspace || !aligned16(workspace)) return TVM_ATTN_INVALID_ARG;
         if (workspace_bytes < norm_bwd_workspace(*p)) return TVM_ATTN_WORKSPACE_TOO_SMALL;
@@ -257,7 +270,7 @@ int tvm_attn_rmsnorm_s8(const tvm_attn_rows_params* p, const tvm_attn_rows* x, c
     c.add(x, &c.k.in[0], true); c.add(res, &c.k.in[1], false);
     c.add(q, &c.k.out[0], true, true); c.add(h, &c.k.out[1], false);
     c.scale(g);
-    if (!c.ok || !s || reinterpret_cast<uintptr_t>(s) % 4) return TVM_ATTN_INVALID_ARG;
+    if (!c.ok || c.overlapping(true) || !s || reinterpret_cast<uintptr_t>(s) % 4) return TVM_ATTN_INVALID_ARG;
     c.k.aux = s;
     c.k.norm = true;
     return launch_norm<ROW_S8>(c, static_cast<cudaStream_t>(cuda_stream));
@@ -270,7 +283,7 @@ int tvm_attn_quantize_s8(const tvm_attn_rows_params* p, const tvm_attn_rows* x, 
     if (c.k.total == 0) return TVM_ATTN_OK;
     c.add(x, &c.k.in[0], true);
     c.add(q, &c.k.out[0], true, true);
-    if (!c.ok || !s || reinterpret_cast<uintptr_t>(s) % 4) return TVM_ATTN_INVALID_ARG;
+    if (!c.ok || c.overlapping(true) || !s || reinterpret_cast<uintptr_t>(s) % 4) return TVM_ATTN_INVALID_ARG;
     c.k.aux = s;
     c.k.eps = 1.f;   // (the sum of squares is not used: nothing is to be scaled for it)
     return launch_norm<ROW_S8>(c, static_cast<cudaStream_t>(cuda_stream));

@@ -69,6 +69,19 @@ def test_strides_and_pointers_of_rows(lib, row, batch, ptr):
     assert lib.tvm_attn_quantize_s8(_params(), bad, _rows(1), 4096, None) == INVALID
 
 
+def test_outputs_on_top_of_one_another_or_of_inputs_that_lie_differently(lib):
+    def fwd(x, y, res=None, h=None):
+        return lib.tvm_attn_rmsnorm_jvp_fwd(_params(), x, res, None, None, None, y, h, None, None, None)
+
+    assert fwd(_rows(0), _rows(2), _rows(1), _rows(2)) == INVALID                    # y and h in one place
+    assert fwd(_rows(0), _rows(0, row=128, batch=1024)) == INVALID                   # y over x, at other strides
+    assert fwd(_rows(0), _rows(1, row=128, batch=1024), _rows(1), _rows(2)) == INVALID
+    back = lambda dx, dtx: lib.tvm_attn_rmsnorm_jvp_bwd(_params(), _rows(0), _rows(1), None, _rows(2), _rows(3), None, None, dx, dtx, None, None, 0, None)  # noqa: E731
+    assert back(_rows(4), _rows(4)) == INVALID and back(_rows(0, row=64, batch=512), _rows(4)) == INVALID
+    assert lib.tvm_attn_quantize_s8(_params(), _rows(0), _rows(0), 4096, None) == INVALID
+    assert lib.tvm_attn_rmsnorm_s8(_params(), _rows(0), _rows(1), None, _rows(1), 4096, _rows(2), None) == INVALID
+
+
 def test_calls_without_rows_need_nothing(lib):
     for p in (dict(B=0), dict(T=0)):
         assert lib.tvm_attn_rmsnorm_jvp_fwd(_params(**p), *[None] * 10) == OK
