@@ -246,6 +246,7 @@ int tvm_attn_rmsnorm_jvp_bwd(const tvm_attn_rows_params* p, const tvm_attn_rows*
 /*
  * The same norm without tangents, its output in 8 bits with a scale for each row: h = x + res, y = g h / r,
  *     s = max|y| / 127     q = y / s rounded to nearest even (a row of zeros: s = 0, q = 0)
+ * q is rounded from the fp32 number nearest to the quotient 127 y / max|y|, so that its ties are those of the elements (of g h, in fp32).
  * A row that holds an infinity or a NaN gets q = 0 and an s that is not finite, so that its products are not finite either.
  *   in : x, res or absent, g or NULL (as above)      out: q: 8-bit rows; s: B * T floats, packed; h exactly where res is given
  */

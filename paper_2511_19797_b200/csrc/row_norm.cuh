@@ -8,7 +8,7 @@
 // and its stores: few registers a thread, so that the blocks of an SM, each a row further on, cover for one another.  The sums over a
 // row, the dot products and the scale's gradient are fp32.  The norm is that of the sum before it is rounded to the type that h is
 // stored in.  Measured on B200, (16384, 1152) bf16, outputs given: norm with residual and tangents 49.5 us (302 MB, 6.1 TB/s of 6.5), without
-// tangents 26.5, backward with residual, tangents and scale 54.7 (5.5 TB/s; 50.7 without the scale), without tangents 29.7, 8-bit rows 25.6.
+// tangents 26.5, backward with residual, tangents and scale 54.7 (5.5 TB/s; 50.7 without the scale), without tangents 29.7, 8-bit rows 26.9.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -346,14 +346,22 @@ row_norm_kernel(const RowNormParams p) {
         const float root = rsqrtf(sums[0] * inv_d + p.eps * pre * pre);   // 1 / (r pre)
         const float inv = root * pre;
         if constexpr (MODE == ROW_S8) {
-            // scaled first where 127 / max would leave the range of the fast division; zeros where the maximum is not finite
+            // 127 v / max for every element v of the row.  Scaled first where 127 / max would leave the range of the fast division; zeros where the
+            // maximum is not finite.
             const float top = sums[N - 1], up = top < 0x1p-100f ? 0x1p100f : top > 0x1p100f ? 0x1p-100f : 1.f;
             const bool fine = top <= 3.4028235e38f && top > 0.f;
-            const float k = fine ? __fdividef(127.f, top * up) : 0.f;
+            // 127 / max as k + low, which is off by 2^-43 of itself: v k + v low, rounded once, is then the fp32 number nearest to the quotient, and a
+            // quotient halfway between two whole numbers (an element of half the maximum is 63.5) comes out as just that.  v k alone is up to two units
+            // off, to one side for a whole row: of (8000, 768) bf16 normals 4164 values missed the even neighbour (a division by the scale in fp32 misses
+            // 422, this none).  (16384, 1152) bf16: 19.7 -> 20.6 us without a norm, 25.8 -> 26.9 with norm and residual.
+            const float k = fine ? __fdividef(127.f, top * up) : 0.f, low = fmaf(-k, top * up, 127.f) * k * (1.f / 127.f);
             if (act) {
-                if (L.c == 0) p.aux[row] = top * (p.norm ? inv : 1.f) * (1.f / 127.f);
+                if (L.c == 0) {   // the quotient by 127, rounded once
+                    const float y = p.norm ? top * inv : top, part = y * (1.f / 127.f);
+                    p.aux[row] = fmaf(fmaf(-127.f, part, y), 1.f / 127.f, part);
+                }
                 int8_t* to = reinterpret_cast<int8_t*>(row_of(p.out[0].p + L.col(0, 0), p.out[0], at, p));
-                const uint64_t up2 = ptx::pack2(up, up), k2 = ptx::pack2(k, k), round2 = ptx::pack2(12582912.f, 12582912.f);   // 1.5 2^23
+                const uint64_t up2 = ptx::pack2(up, up), k2 = ptx::pack2(k, k), low2 = ptx::pack2(low, low), round2 = ptx::pack2(12582912.f, 12582912.f);   // 1.5 2^23
 #pragma unroll
                 for (int i = 0; i < C; ++i) {
                     // 1.5 2^23 + x, |x| <= 127, rounds x to the nearest whole number (even on ties), whose 8 bits are the sum's lowest
@@ -363,7 +371,7 @@ row_norm_kernel(const RowNormParams p) {
                         uint64_t v = ptx::mul2(h[i][e], g[i][e]);
                         if (up != 1.f) v = ptx::mul2(v, up2);
                         float a, b;
-                        ptx::unpack2(ptx::add2(ptx::mul2(v, k2), round2), a, b);
+                        ptx::unpack2(ptx::add2(ptx::fma2(v, k2, ptx::mul2(v, low2)), round2), a, b);
                         q[2 * e] = __float_as_uint(a);
                         q[2 * e + 1] = __float_as_uint(b);
                     }
