@@ -229,10 +229,16 @@ __device__ __forceinline__ void clear_slots(float* slots, int n) {
     __syncthreads();
 }
 
-// The power of two that a row's elements are multiplied by in its sum of squares, when that sum left the range of fp32 at `pre` =
-// 1: a second sum is then taken.  0: the sum is fine.  (With eps of ordinary size a row of tiny elements needs none.)
-__device__ __forceinline__ float row_rescale(float ss, float eps) {
-    return !(ss <= 3.0e38f) ? 0x1p-64f : ss < 1e-30f && eps < 1e-30f ? 0x1p64f : 0.f;
+// Rows whose sum of squares leaves the range of fp32, or comes near its ends, are summed again with their elements multiplied by a power of
+// two.  (With eps of ordinary size a row of tiny elements needs none.)  The first factor brings every such sum into the range (the largest
+// element, 2^42 to 2^128 or 2^-149 to 2^-49, to 2^-54 to 2^47); the second one, from what the first sum says, makes r about 2^aim.
+__device__ __forceinline__ bool row_leaves(float ss, float eps) { return !(ss <= 1e30f) || (ss < 1e-30f && eps < 1e-30f); }
+__device__ __forceinline__ float row_first(float ss) { return ss < 1e-30f ? 0x1p96f : 0x1p-96f; }
+// `ms`: r^2 of elements multiplied by `first`.  1 where there is nothing to be brought back: a row of zeros, an infinity or a NaN.
+__device__ __forceinline__ float row_power(float first, float ms, int aim) {
+    if (!(ms > 0.f && ms <= 3.4028235e38f)) return 1.f;
+    const int n = (first < 1.f ? -96 : 96) + aim - (((int)(__float_as_uint(ms) >> 23) - 127) >> 1);   // -144 to 127
+    return __uint_as_float(n >= 127 ? 254u << 23 : n >= -126 ? (uint32_t)(n + 127) << 23 : 1u << (n + 149));
 }
 
 // ROW_NORM: y (h, ty, th).  ROW_NORM_TAN: with tangents.  ROW_S8: 8-bit rows q = rint(v / s), s = max|v| / 127, of v = y or x + res;
@@ -314,17 +320,17 @@ row_norm_kernel(const RowNormParams p) {
                     }
                 }
         }
-        // sums[0] = h . h, sums[1] = h . th or max |g h|; h times `pre` in the first two
-        float sums[N], pre = 1.f;
+        // sums[0] = h . h, sums[1] = h . th or max |g h|; h times `dn` in the first two
+        float sums[N], dn = 1.f, eps = p.eps;
         auto sum_up = [&](bool scaled) {
-            const uint64_t pre2 = ptx::pack2(pre, pre);
+            const uint64_t dn2 = ptx::pack2(dn, dn);
             uint64_t ss2 = 0ull, s2 = 0ull;
             float top = 0.f;
 #pragma unroll
             for (int i = 0; i < C; ++i)
 #pragma unroll
                 for (int e = 0; e < V / 2; ++e) {
-                    const uint64_t x = scaled ? ptx::mul2(h[i][e], pre2) : h[i][e];
+                    const uint64_t x = scaled ? ptx::mul2(h[i][e], dn2) : h[i][e];
                     if (MODE != ROW_S8 || p.norm) ss2 = ptx::fma2(x, x, ss2);
                     if constexpr (TAN) s2 = ptx::fma2(x, t[i][e], s2);
                     if constexpr (MODE == ROW_S8) {
@@ -338,13 +344,28 @@ row_norm_kernel(const RowNormParams p) {
             row_reduce<N, MODE == ROW_S8, BLOCK>(sums, p.P, slots + (BLOCK ? (turn++ & 1u) * 32 * N : 0));
         };
         sum_up(false);
-        const float again = row_rescale(sums[0], p.eps);
-        if (BLOCK ? again != 0.f : __any_sync(0xffffffffu, again != 0.f)) {   // (the rows of the warp that need none keep pre = 1)
-            pre = again != 0.f ? again : 1.f;
+        const bool leaves = row_leaves(sums[0], eps);
+        if (BLOCK ? leaves : __any_sync(0xffffffffu, leaves)) {   // (the other rows of the warp are multiplied by 1)
+            if (leaves) dn = row_first(sums[0]);
+            sum_up(true);
+            const float all = leaves ? row_power(dn, sums[0] * inv_d + eps * dn * dn, -16) : 1.f;
+            // y, ty and 8-bit values are those of h and th both multiplied by `all`.  Where that is above 1 they are: nothing is rounded, and 1 / r may be beyond
+            // the range.  Below 1 small elements would be lost, which only the 8-bit values allow, so there the factor stays with the sums.
+            const float up = MODE == ROW_S8 ? all : fmaxf(all, 1.f);
+            const uint64_t up2 = ptx::pack2(up, up);
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+#pragma unroll
+                for (int e = 0; e < V / 2; ++e) {
+                    h[i][e] = ptx::mul2(h[i][e], up2);
+                    if constexpr (TAN) t[i][e] = ptx::mul2(t[i][e], up2);
+                }
+            dn = MODE == ROW_S8 ? 1.f : fminf(all, 1.f);
+            eps = eps * all * all;
             sum_up(true);
         }
-        const float root = rsqrtf(sums[0] * inv_d + p.eps * pre * pre);   // 1 / (r pre)
-        const float inv = root * pre;
+        const float root = rsqrtf(sums[0] * inv_d + eps);   // 1 / (r dn)
+        const float inv = root * dn;
         if constexpr (MODE == ROW_S8) {
             // 127 v / max for every element v of the row.  Scaled first where 127 / max would leave the range of the fast division; zeros where the
             // maximum is not finite.
@@ -394,7 +415,7 @@ row_norm_kernel(const RowNormParams p) {
                 }
             }
         } else if (act) {
-            const float m = TAN ? sums[N - 1] * root * root * inv_d * pre : 0.f;   // (u . th) / (D r): th . h pre is known
+            const float m = TAN ? sums[N - 1] * inv_d * root * inv : 0.f;   // (u . th) / (D r): th . h dn is known, whose mean is in the range where th is
             const uint64_t inv2 = ptx::pack2(inv, inv), nm2 = ptx::pack2(-m, -m);
             T* y = L.template at<false>(p.out[0], at, p);
             T* ty = TAN ? L.template at<false>(p.out[2], at, p) : nullptr;
@@ -518,9 +539,9 @@ row_norm_bwd_kernel(const RowNormParams p) {
             row_reduce<N, false, BLOCK>(s, p.P, slots + (BLOCK ? (turn++ & 1u) * 32 * N : 0));
         };
         sum_up(false);
-        const float again = row_rescale(s[0], p.eps);
-        if (BLOCK ? again != 0.f : __any_sync(0xffffffffu, again != 0.f)) {
-            pre = again != 0.f ? again : 1.f;
+        const bool leaves = row_leaves(s[0], p.eps);
+        if (BLOCK ? leaves : __any_sync(0xffffffffu, leaves)) {
+            if (leaves) pre = row_first(s[0]);
             sum_up(true);
         }
         const float root = rsqrtf(s[0] * inv_d + p.eps * pre * pre), inv = root * pre;
