@@ -510,7 +510,7 @@ row_norm_bwd_kernel(const RowNormParams p) {
         };
         // Ends the reuse of an earlier unpacking across the reductions.
         auto keep = [](uint4& q) { asm volatile("" : "+r"(q.x), "+r"(q.y), "+r"(q.z), "+r"(q.w)); };
-        // h.h, a.h, then with tangents h.th, b.h, b.th; h times `pre`
+        // h.h, a.h, then with tangents h.th, b.h, b.th; h, and th in the last one, times `pre`
         float s[N], pre = 1.f;
         auto sum_up = [&](bool scaled) {
             const uint64_t pre2 = ptx::pack2(pre, pre);
@@ -530,7 +530,7 @@ row_norm_bwd_kernel(const RowNormParams p) {
                         const uint64_t b = ptx::mul2(g[e], z[e]);
                         acc[2] = ptx::fma2(x, t[e], acc[2]);
                         acc[3] = ptx::fma2(b, x, acc[3]);
-                        acc[4] = ptx::fma2(b, t[e], acc[4]);
+                        acc[4] = ptx::fma2(b, scaled ? ptx::mul2(t[e], pre2) : t[e], acc[4]);
                     }
                 }
             }
@@ -543,22 +543,21 @@ row_norm_bwd_kernel(const RowNormParams p) {
         if (BLOCK ? leaves : __any_sync(0xffffffffu, leaves)) {
             if (leaves) pre = row_first(s[0]);
             sum_up(true);
+            // large rows so that h . th stays in the range, tiny ones so that products with cotangents of their size do
+            if (leaves) pre = row_power(pre, s[0] * inv_d + p.eps * pre * pre, pre < 1.f ? -16 : 16);
+            sum_up(true);
         }
-        const float root = rsqrtf(s[0] * inv_d + p.eps * pre * pre), inv = root * pre;
-        const float au = s[1] * root;
-        // dx = inv a + kh u + kb b + kt th, dtx = inv b + zh u;  u = h inv
-        float kh = -inv * au * inv_d, kb = 0.f, kt = 0.f, zh = 0.f, jt = 0.f;
+        const float root = rsqrtf(s[0] * inv_d + p.eps * pre * pre), inv = root * pre;   // 1 / (r pre), 1 / r
+        // dx = inv (a + jt b + zh th) + kh u, dtx = inv b + zh u, J th = inv th + jt u;  u = h inv.  No factor has 1 / r^2 or a sum of products that
+        // may leave the range (u . a does where its mean and dx do not).
+        float kh = -inv * (s[1] * inv_d * root), zh = 0.f, jt = 0.f;
         if constexpr (TAN) {
-            const float ut = s[2] * root, bu = s[3] * root, f = inv * inv * inv_d;
-            kh += f * (3.f * bu * ut * inv_d - s[4]);
-            kb = -f * ut;
-            kt = -f * bu;
-            zh = -inv * bu * inv_d;
-            jt = -inv * ut * inv_d;
+            zh = -inv * (s[3] * inv_d * root);
+            jt = -inv * (s[2] * inv_d * root);
+            kh += 3.f * zh * jt - s[4] * inv_d * root * inv;
         }
         if (act) {
-            const uint64_t inv2 = ptx::pack2(inv, inv), kh2 = ptx::pack2(kh, kh), kb2 = ptx::pack2(kb, kb), kt2 = ptx::pack2(kt, kt);
-            const uint64_t zh2 = ptx::pack2(zh, zh), jt2 = ptx::pack2(jt, jt);
+            const uint64_t inv2 = ptx::pack2(inv, inv), kh2 = ptx::pack2(kh, kh), zh2 = ptx::pack2(zh, zh), jt2 = ptx::pack2(jt, jt);
             T* dx = L.template at<SAME>(p.out[0], at, p);
             T* dtx = TAN ? L.template at<SAME>(p.out[1], at, p) : nullptr;
 #pragma unroll
@@ -576,15 +575,16 @@ row_norm_bwd_kernel(const RowNormParams p) {
                 unpack(i, h, y, t, z, g);
 #pragma unroll
                 for (int e = 0; e < V / 2; ++e) {
-                    const uint64_t u = ptx::mul2(h[e], inv2), a = ptx::mul2(g[e], y[e]);
-                    ox[e] = ptx::fma2(a, inv2, ptx::fma2(u, kh2, ox[e]));
+                    const uint64_t u = ptx::mul2(h[e], inv2);
+                    uint64_t a = ptx::mul2(g[e], y[e]);
                     dg[i][e] = ptx::fma2(y[e], u, dg[i][e]);
                     if constexpr (TAN) {
                         const uint64_t b = ptx::mul2(g[e], z[e]);
-                        ox[e] = ptx::fma2(b, kb2, ptx::fma2(t[e], kt2, ox[e]));
+                        a = ptx::fma2(t[e], zh2, ptx::fma2(b, jt2, a));
                         ot[e] = ptx::fma2(b, inv2, ptx::fma2(u, zh2, ot[e]));
                         dg[i][e] = ptx::fma2(z[e], ptx::fma2(t[e], inv2, ptx::mul2(u, jt2)), dg[i][e]);
                     }
+                    ox[e] = ptx::fma2(a, inv2, ptx::fma2(u, kh2, ox[e]));
                 }
                 L.store(dx, i, ox);
                 if constexpr (TAN) L.store(dtx, i, ot);

@@ -1,5 +1,5 @@
-"""Rows whose squares leave the range of fp32, next to ordinary rows of the same warp: norm, tangent and 8-bit rows against the fp64
-oracle, with the bounds of the ordinary ones (64 roundings).
+"""Rows whose squares leave the range of fp32, next to ordinary rows of the same warp: norm, tangent, 8-bit rows and backward against the
+fp64 oracle, with the bounds of the ordinary ones (64 roundings, 128 for the scale's gradient).
 
 The factor that brings a row back is a power of two, exact in itself; 1 / r beyond 2^126 is a denormal number, off by up to 2^-22 of itself, which is
 four roundings more for each of the two such factors that enter a result: the 64 have room for them (sums of at most 40 elements a thread and 10
@@ -68,3 +68,23 @@ def test_8_bits(D, dtype, sizes):
         for scale in (g, None, 100 * g):          # (the scaled sum itself leaves the range)
             q, s, _ = binding.tvm_attn_rmsnorm_s8(*_dev(x, None, scale), eps=eps)
             _check_8_bits(q, s, orn.rmsnorm_jvp_fwd(*map(_np, (x, None, None, None, scale)), eps)["y"][0])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", WIDTHS)
+@pytest.mark.parametrize("sizes", [LARGE, TINY])
+def test_backward(D, dtype, sizes):
+    h, g = _rows(D, D, dtype, sizes), 1 + _draw(D + 9, D, std=0.3)
+    # cotangents of the size of the rows give dx and dtx of order one; 2^-20 of it where their sum over the rows would leave the range
+    like = [s * 2.0 ** -20 if s > 1e19 else s for s in sizes]
+    dy, dty = _rows(D + 1, D, dtype, like), _rows(D + 2, D, dtype, like)
+    near, ordinary = _rows(D + 3, D, dtype, sizes), _rows(D + 4, D, dtype, [1.0 if s > 1e-15 else s for s in sizes])
+    dh, dth = (_rows(D + 5 + k, D, dtype, [1.0] * len(sizes)) for k in range(2))
+    for eps in (0.0, 1e-6):
+        for ins in ((h, dy, None, None, None, None), (h, dy, near, dty, None, None), (h, dy, ordinary, dty, dh, dth), (h, torch.zeros_like(dy), near, dty, None, dth)):
+            for scale in (g, None):
+                got = binding.tvm_attn_rmsnorm_jvp_bwd(*_dev(*ins, scale), eps=eps)
+                want = orn.rmsnorm_jvp_bwd(*map(_np, (*ins, scale)), eps)
+                for name, v in zip(("dx", "dtx", "dg"), got):
+                    if v is not None:
+                        _close(v, want[name], 128 if name == "dg" else 64, what=(name, eps))
