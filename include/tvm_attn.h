@@ -230,7 +230,8 @@ int tvm_attn_rmsnorm_jvp_fwd(const tvm_attn_rows_params* p, const tvm_attn_rows*
  * Backward through all outputs of tvm_attn_rmsnorm_jvp_fwd.  With the cotangents dy, dty of y, ty and dh, dth of h, th:
  *     dtx = J (g * dty) + dth     dx = J (g * dy) + d/dh [ (g * dty) . (J(h) th) ] + dh
  *     dg = sum over the rows of dy * u + dty * (J th)
- * dx is the gradient of x and of res, dtx that of tx and of tres.
+ * dx is the gradient of x and of res, dtx that of tx and of tres.  Rows whose squares leave the range of fp32 are scaled as in the forward; 1 / r has to be
+ * in it (r >= 2^-126).
  *   in : h (what the forward wrote, or its x without a residual); dy; dh or absent (zero);
  *        th and dty, both or neither (neither: no tangents, or a loss that does not use ty); dth or absent, only with th
  *   out: dx; dtx exactly where th is given; dg: D floats exactly where g is given, written, bit-reproducible

@@ -9,13 +9,15 @@
 // the tensor cores.  Warp 0 loads by TMA, warp 1 of the pair's first CTA issues the MMAs, warps 4 to 11 scale and store one
 // accumulator while the other one fills; a pair walks over its tiles, and the ring of loads runs on through them.
 //
-// Up to 256 rows the weights' bytes are what a product costs, and they stream past the tokens: the weights are then the tensor cores'
-// operand with 128 rows, and the CTAs of a cluster share k.  Up to 2 rows (single tokens) dp4a on operands that go from global memory
+// Up to 256 rows the weights' bytes are what a product costs.  There the weights can be the tensor cores' operand with 128 rows and stream past the
+// tokens, the CTAs of a cluster sharing k; that is done where it is faster than tiles of 256 rows (14336 x 4096 weights: up to 57 tokens, 4096 x
+// 14336: always; the rule and its times stand at linear() in row_ops_api.cu).  Up to 2 rows (single tokens) dp4a on operands that go from global memory
 // straight to registers keeps pace with HBM: nothing is set up, and nothing waits.  (mma.sync, which emulates 8-bit products on this
 // GPU at some 150 multiply-adds a cycle and SM, took 20 us for one token and 14336 x 4096 weights.)
 //
 // Measured on B200: 16384 x 3456 x 1152, bf16 out, 52 us in bursts and 61 at the power cap (2.1 Pop/s), 16384 x 4608 x 9216 421 (3.3 Pop/s, bursts), output
-// alone (K = 128) at the rate of a fill; one token against 14336 x 4096 11.6 us (5 TB/s), 28672 x 4096 20.3 (5.8), 16 tokens 14.3, 64 tokens 18.
+// alone (K = 128) at the rate of a fill; one token against 14336 x 4096 11.6 us (5 TB/s), 28672 x 4096 20.3 (5.8), 16 tokens 13.9; 64
+// and 256 tokens, in tiles of 256 rows on 112 SMs, 17.5 and 18.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -64,8 +66,9 @@ __device__ __forceinline__ uint4 linear_load16(const int8_t* row, int k, int K, 
     return v;
 }
 
-// Up to MT tokens, R channels a warp; the lanes share k.  All warps are resident at once: what an SM has more of than others costs
-// nothing, since HBM is the bound and not the SM.
+// Up to MT tokens, R channels a warp; the lanes share k.  Up to some 21000 channels (R = 4: nine blocks of 128 threads an SM) all warps are resident at
+// once, and what an SM has more of than others costs nothing, since HBM is the bound and not the SM; beyond that blocks follow as others end
+// (28672 x 4096 keeps 5.8 TB/s).
 template <typename OUT, int MT, int R>
 __global__ void __launch_bounds__(LIN_FEW_THREADS) linear_s8_few_kernel(const LinearParams p) {
     constexpr int U = LIN_FEW_LOADS / R;
@@ -393,7 +396,7 @@ linear_s8_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__
 // ------------------------------------------------------------------------------------------------ some rows
 // Up to 256 rows: the weights stream past the tokens, so they are the operand with 128 rows (channels), the tokens the one with NT columns,
 // and the cluster's CTAs share k.  When all are done, each writes its partial sums, integers, of a token into the shared memory of the
-// CTA that adds them up (writes do not wait for one another; fetched by reads, 64 tokens took 4 us more).  Up to 64 tokens three
+// CTA that adds them up (writes do not wait for one another; fetched by reads, 64 tokens took 4 us more).  Tiles of up to 64 tokens have three
 // CTAs an SM: what it has in flight is 150 KB and more.
 constexpr int LIN_THIN_THREADS = 192;
 

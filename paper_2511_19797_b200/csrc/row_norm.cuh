@@ -7,8 +7,8 @@
 // each of P lanes of a warp, or 1, 2 or 4 chunks on each thread of a block of its own, and stays in registers between its loads
 // and its stores: few registers a thread, so that the blocks of an SM, each a row further on, cover for one another.  The sums over a
 // row, the dot products and the scale's gradient are fp32.  The norm is that of the sum before it is rounded to the type that h is
-// stored in.  Measured on B200, (16384, 1152) bf16, outputs given: norm with residual and tangents 49.5 us (302 MB, 6.1 TB/s of 6.5), without
-// tangents 26.5, backward with residual, tangents and scale 54.7 (5.5 TB/s; 50.7 without the scale), without tangents 29.7, 8-bit rows 26.9.
+// stored in.  Measured on B200, (16384, 1152) bf16, outputs given: norm with residual and tangents 50 us (302 MB, 6.0 TB/s of 6.5), without
+// tangents 26.9, backward with residual, tangents and scale 54.5 (5.5 TB/s), without tangents 29.3, 8-bit rows 27.0, without a norm 20.1.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -38,12 +38,16 @@ struct RowNormParams {
 };
 
 constexpr int ROWNORM_THREADS = 256;   // of a block whose rows are on warps
-constexpr int ROWNORM_SINGLE = 160;    // chunks of a row with one on each thread, at most
+// Chunks of a row with one on each thread, at most: two a thread from there on.  The backward sets it (the norms differ by 5 % at most between 96 and 256): with
+// tangents and 38 MB a tensor of bf16 rows, 1152 wide 53.9 us as it is, 63.8 with two chunks a thread (a limit of 128); 1408 wide 58.6 as it is and 55.9 with one
+// (a limit of 192), but then all blocks are compiled for 192 threads and fewer registers each, and 1152 wide takes 58.1, 512 wide 90.8 instead of 81.2.
+constexpr int ROWNORM_SINGLE = 160;
 // Threads that a block with one row can have, C chunks each.
 template <typename T, int C> constexpr int rownorm_block_threads() { return C == 4 && sizeof(T) == 4 ? 1024 : C == 1 ? ROWNORM_SINGLE : 512; }
 // Blocks of the backward on an SM: as many as the registers let in (a block walks over its rows from the start to the end of the
-// launch, so one that waits for another's end would double the time).  `threads`: of a block with one row of C chunks a thread, 0 for
-// rows on warps.
+// launch, so one that waits for another's end would double the time), of one chunk a thread those of ROWNORM_SINGLE threads, whatever their own
+// number: narrower ones leave registers unused (512 wide with tangents 81 us where 1152 take 54).  `threads`: of a block with one row of C chunks a
+// thread, 0 for rows on warps.
 __host__ __device__ constexpr int rownorm_bwd_resident(int threads, int C, bool tan) {
     return threads == 0 ? (tan ? 2 : 4) : C == 1 ? (tan ? 4 : 7) : threads <= 512 ? 512 / threads : 1;
 }

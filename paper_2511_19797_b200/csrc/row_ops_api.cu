@@ -154,8 +154,10 @@ template <typename T, int MODE>
 static int launch_norm(const RowsCall& c, cudaStream_t st) {
     const DeviceFacts* dev = device_facts();
     if (!dev) return TVM_ATTN_CUDA_ERROR;
-    // 8-bit rows, whose work per row weighs most, with two chunks a thread from 65 chunks on: it is then that of fewer warps ((16384, 1152) bf16
-    // 26.3 -> 24.9 us, without a norm 21.2 -> 19.2).  (The norm with tangents 49.6 -> 51.6; without them, which gives the same bits, 26.5 -> 26.4.)
+    // 8-bit rows, whose work per row weighs most, with two chunks a thread from 65 chunks on: it is then that of fewer warps.  Without a norm, 38 MB of bf16
+    // rows, one chunk a thread and two: 1280 wide 21.9, 18.5 us, 1152 23.8, 20.1, 1024 19.3, 16.2; 768 19.6, 20.5;
+    // 512 21.8, 16.3, 272 38.5, 27.5, where two would be the faster too.  With norm and residual alike (1152 30.0, 27.0).
+    // (The norm with tangents, 1152 wide, 49.6 and 51.6.)
     const RowSplit split = row_split(c.k.D, sizeof(T), MODE == ROW_S8 ? 64 : ROWNORM_SINGLE);
     RowNormParams k = c.k;
     k.P = split.P;
@@ -349,7 +351,8 @@ static int launch_many(LinearParams p, const DeviceFacts& dev, cudaStream_t st) 
 // Cycles of a product in tiles of 256 rows, and the width of a tile: the one whose rounds of tiles take least.  Narrow tiles load more for what
 // they compute: 128 bytes of k took 776, 624, 546 and 484 cycles with 256, 192, 128 and 64 channels (K = 9216, four tiles a pair, of a clock that the power
 // cap lowers), in proportion to 256 + BN.  16384 x 3456 x 1152 51.9, 54.4, 65.8, 109.8 us; 8000 x 768 x 768 10.5, 9.6, 10.8, 15.6; 512 x 4608 x 1152 9.5,
-// 8.5, 7.6, 11.0.  -1: more tiles than there can be.
+// 8.5, 7.6, 11.0.  (Widths are compared with one another, for which the factor does not matter; 6/5 of a cycle, less than a stage takes in a long product,
+// puts the crossing with thin_cycles where the times in linear() have it.)  -1: more tiles than there can be.
 static long long many_cycles(const LinearParams& p, const DeviceFacts& dev, int* width) {
     const long long tiles_m = (p.M + 2 * LIN_ROWS - 1) / (2 * LIN_ROWS), pairs = dev.sms / 2, kblocks = (p.K + 127) / 128;
     if (tiles_m * ((p.N + 63) / 64) > 2147483647LL) return -1;
@@ -405,9 +408,10 @@ static int linear(LinearParams p, cudaStream_t st) {
     int bn = 0;
     const long long many = many_cycles(p, *dev, &bn);
     if (p.M <= 256) {
-        // Weights past the tokens, k shared by as many CTAs as is fastest, where that beats tiles of 256 rows.  Estimates of both in
-        // thousands of cycles, times in us (thin, many): 128 tokens x (4096 x 14336) 24, 43: 23.7, 30.5; x (1152 x 4608) 8, 14: 10.3, 14.4; x (14336 x
-        // 4096) 32, 20: 23.7, 22.6; x (4608 x 1152) 11, 4: 18.7, 8.3; 16 tokens x (4608 x 1152) 2.3, 3.5: 8.3, 8.3 to 10.3.
+        // Weights past the tokens, k shared by as many CTAs as is fastest, where that beats tiles of 256 rows by the two estimates.  Times in us (thin,
+        // many) and what is taken: tokens x (14336 x 4096) 48: 16.3, 17.5 thin; 56: 17.3, 17.5 thin; 58: 17.3, 17.5 many; 64: 17.9, 17.5 many; 128: 32.8, 17.8
+        // many; x (4096 x 14336) 64: 17.7, 27.2 thin; 256: 24.9, 27.7 thin; x (4608 x 1152) 32: 6.7, 7.0 thin; 48: 8.6, 7.0 many; x (1152 x 4608) 192: 11.7, 11.7
+        // many; 256: 14.3, 11.8 many; x (768 x 768) 32: 4.7, 5.5 thin; 48: 4.9, 5.6 many, the one of these where the other was faster; 96: 6.5, 5.8 many.
         const int kblocks = (p.K + 127) / 128;
         // up to 64 tokens three CTAs of an SM together keep enough of the weights in flight: as many share k as are resident (two of them, 14336 x
         // 4096: 18.6 instead of 16.5 us); then the number of them that is fastest
