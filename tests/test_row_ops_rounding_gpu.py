@@ -77,3 +77,17 @@ def test_fp32_rows(D):
     q, s = binding.tvm_attn_quantize_s8(x.cuda())
     assert (np.abs(q.cpu().double().numpy() - _steps(x)) <= 0.5 + 2.0 ** -18 + 2.0 ** -30).all()
     assert np.array_equal(s.cpu().numpy(), x.abs().amax(-1).numpy() / np.float32(127))
+
+
+@pytest.mark.parametrize("dtype,step", [(torch.bfloat16, 2.0 ** -133), (torch.float32, 2.0 ** -149), (torch.float32, 2.0 ** 121)])
+@pytest.mark.parametrize("D", [127, 256])
+def test_rows_of_the_smallest_and_the_largest_numbers(dtype, step, D):
+    """Whole multiples of the type's smallest number (denormal), up to 127 of it, and of one next to its largest."""
+    top = torch.arange(1, 128, dtype=torch.float64)[:, None]
+    x = (torch.minimum(torch.arange(D, dtype=torch.float64)[None, :] % 127 + 1, top) * step).to(dtype)
+    q, s = binding.tvm_attn_quantize_s8(x.cuda())
+    assert np.array_equal(q.cpu().numpy(), np.rint(_steps(x)))
+    # a scale below 2^-126 has fewer bits: within one of them
+    assert (np.abs(s.cpu().double().numpy() - top[:, 0].numpy() * step / 127) <= np.maximum(top[:, 0].numpy() * step / 127 * 2.0 ** -24, 2.0 ** -149)).all()
+    q8, _, _ = binding.tvm_attn_rmsnorm_s8(x.cuda(), eps=0.0)
+    assert np.array_equal(q8.cpu().numpy(), np.rint(_steps(x)))
